@@ -286,6 +286,82 @@ oc_status oc_layer_cached(const oc_shape *shape, const oc_cfg *cfg, const void *
 oc_status oc_residual_add(const oc_shape *shape, const void *x, const void *y, void *h, hipStream_t stream);
 
 /*
+ * Norms before and after a sublayer, fused with its gate, its modulation and
+ * the residual.  Around a denoiser's sublayer (attention or feed-forward) the
+ * residual stream x and the sublayer's output y become the next stream h and
+ * the next sublayer's input n:
+ *   z = post(y),  h = res_scale * x + gate * z,
+ *   n = pre(h) * (1 + scale) + shift.
+ */
+typedef enum {
+    OC_NORM_NONE = 0,         /* v                                                          */
+    OC_NORM_RMS = 1,          /* v / sqrt(mean(v^2) + eps)                                  */
+    OC_NORM_LAYER = 2         /* (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps)          */
+} oc_norm_kind;
+
+typedef struct {
+    int32_t kind;             /* oc_norm_kind, over the C channels of a row                 */
+    float   eps;              /* finite, >= 0                                               */
+    const void *w, *b;        /* [C] weights and biases applied after it; NULL: 1 and 0     */
+} oc_norm;
+
+typedef struct {
+    const void *gate;         /* [n_mod, C] or NULL (1)                                     */
+    const void *scale;        /* [n_mod, C] or NULL (0)                                     */
+    const void *shift;        /* [n_mod, C] or NULL (0)                                     */
+    int64_t ld;               /* elements from one modulation row to the next (>= C; the
+                                 vectors may be columns of one wider product)               */
+    int32_t rows_per_mod;     /* >= 1: row r uses modulation row r / rows_per_mod (n_rows:
+                                 one for all; N: one per frame; 1: one per row), so
+                                 n_mod = ceil(n_rows / rows_per_mod)                        */
+    int32_t reserved;         /* must be 0                                                  */
+} oc_mod;
+
+/*
+ * oc_norm_gate — the formulas above for n_rows rows of C channels (shape gives
+ * C and the element type of every tensor; its F, H, W are not used, so text
+ * tokens are rows like any other).  y NULL: no sublayer output, h is x itself
+ * (then post, gate and res_scale must be absent: NULL, NULL, 1) and h must be
+ * NULL; otherwise h NULL: not wanted.  n NULL: not wanted.  post, pre and mod
+ * may be NULL (no norm, no modulation).  x, y, h and n are [n_rows, C]
+ * contiguous; h and n may each be x or y themselves (in place), and overlap
+ * nothing otherwise.  Everything is computed in fp32 (the mean before the
+ * squared deviations) and each output is rounded once: n comes from the
+ * unrounded h.  A NaN or an infinity stays inside its row.
+ * C a multiple of 8; n_rows >= 0 (0: nothing happens).
+ */
+oc_status oc_norm_gate(const oc_shape *shape, int32_t n_rows, const void *x, const void *y, const oc_norm *post,
+                       const oc_norm *pre, const oc_mod *mod, float res_scale, void *h, void *n,
+                       hipStream_t stream);
+
+/*
+ * oc_norm_gate_grad — the gradient of oc_norm_gate: from dh and dn, the
+ * gradients of h and n (either may be NULL: zero; not both), those of x (dx)
+ * and y (dy), [n_rows, C] each, in the tensors' type; and in fp32 those of the
+ * vectors: gate, scale, shift [n_mod, C] (contiguous) and the norms' w and b
+ * [C].  Each output may be NULL (not wanted), and must be where what it
+ * belongs to is NULL.  x, y, post, pre, mod and res_scale are those of the
+ * forward call; statistics, h and z are computed again from x and y, nothing
+ * has to be kept.  Where y is NULL, dh is added to dx.  Sums over rows are
+ * fp32 and taken in an order that depends on the sizes only.  No output may
+ * overlap an input or another output.
+ * ws_bytes >= oc_norm_gate_grad_workspace_bytes(shape, n_rows, rows_per_mod)
+ * (rows_per_mod of mod, or 0 without one).
+ */
+typedef struct {
+    float *gate, *scale, *shift;   /* [n_mod, C] */
+    float *post_w, *post_b;        /* [C]        */
+    float *pre_w, *pre_b;          /* [C]        */
+} oc_norm_grads;
+
+oc_status oc_norm_gate_grad(const oc_shape *shape, int32_t n_rows, const void *x, const void *y, const oc_norm *post,
+                            const oc_norm *pre, const oc_mod *mod, float res_scale, const void *dh, const void *dn,
+                            void *dx, void *dy, const oc_norm_grads *grads, void *ws, size_t ws_bytes,
+                            hipStream_t stream);
+
+size_t oc_norm_gate_grad_workspace_bytes(const oc_shape *shape, int32_t n_rows, int32_t rows_per_mod);
+
+/*
  * oc_block_cached — one spatial + temporal block of a video denoiser with all
  * three caches at once (§3.2: Frame and Token Cache on the spatial layer,
  * Block Cache on the temporal layer; §4.2 runs them together at ratios

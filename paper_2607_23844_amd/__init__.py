@@ -36,3 +36,10 @@ from .api import (  # noqa: F401
     static_scratch_bytes,
     workspace,
 )
+from .ops import (  # noqa: F401
+    Mod,
+    Norm,
+    norm_gate,
+    norm_gate_grad,
+    norm_gate_grad_workspace_bytes,
+)

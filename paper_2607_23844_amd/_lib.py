@@ -12,6 +12,7 @@ OC_OK, OC_ERR_INVALID_ARG, OC_ERR_SHAPE, OC_ERR_DTYPE, OC_ERR_WORKSPACE, OC_ERR_
 OC_F32, OC_BF16 = 0, 1
 GRANS = {"token": 0, "frame": 1, "block": 2, "frame_token": 3}
 COLDS = {"matched": 0, "full": 1}
+NORMS = {"none": 0, "rms": 1, "layer": 2}
 
 
 class OmniCacheError(RuntimeError):
@@ -54,6 +55,20 @@ class oc_ffn_weights(C.Structure):
     _fields_ = [("w1", C.c_void_p), ("w2", C.c_void_p), ("hidden", C.c_int32), ("reserved", C.c_int32)]
 
 
+class oc_norm(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("eps", C.c_float), ("w", C.c_void_p), ("b", C.c_void_p)]
+
+
+class oc_mod(C.Structure):
+    _fields_ = [("gate", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p), ("ld", C.c_int64),
+                ("rows_per_mod", C.c_int32), ("reserved", C.c_int32)]
+
+
+class oc_norm_grads(C.Structure):
+    _fields_ = [("gate", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p), ("post_w", C.c_void_p),
+                ("post_b", C.c_void_p), ("pre_w", C.c_void_p), ("pre_b", C.c_void_p)]
+
+
 class oc_cache_entry(C.Structure):
     _fields_ = [("layer", C.c_int32), ("step", C.c_int32), ("interval", C.c_int32)]
 
@@ -88,6 +103,12 @@ _SIGS = {
                                       C.c_int32, P(oc_cache_entry), C.c_int32, P(C.c_int32), P(C.c_double),
                                       P(C.c_double)]),
     "oc_residual_add": (C.c_int, [P(oc_shape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "oc_norm_gate": (C.c_int, [P(oc_shape), C.c_int32, C.c_void_p, C.c_void_p, P(oc_norm), P(oc_norm), P(oc_mod),
+                               C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "oc_norm_gate_grad": (C.c_int, [P(oc_shape), C.c_int32, C.c_void_p, C.c_void_p, P(oc_norm), P(oc_norm),
+                                    P(oc_mod), C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                    P(oc_norm_grads), C.c_void_p, C.c_size_t, C.c_void_p]),
+    "oc_norm_gate_grad_workspace_bytes": (C.c_size_t, [P(oc_shape), C.c_int32, C.c_int32]),
     "oc_block_cached": (C.c_int, [P(oc_shape), P(oc_cfg), P(oc_cfg), C.c_void_p, P(oc_attn_weights),
                                   P(oc_attn_weights), P(oc_cache), P(oc_cache), C.c_void_p, P(oc_trace), P(oc_trace),
                                   C.c_void_p, C.c_size_t, C.c_void_p]),

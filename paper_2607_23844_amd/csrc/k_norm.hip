@@ -1,0 +1,405 @@
+// Norms before and after a sublayer, fused with its gate, its modulation and
+// the residual, and their gradients.
+//   z = post(y), h = rs x + g z, n = pre(h)(1 + s) + t
+// With u the normalised h (rstd r), a = u w + b its weighted form, v and r_y
+// the same of y, the gradients are
+//   ds = sum dn a, dt = sum dn, da = dn (1 + s), dw = sum da u, db = sum da,
+//   H  = dh + r (da w - m1 - u m2), m2 = mean(da w u), m1 = mean(da w) (layer; 0 for rms),
+//   dx = rs H, dg = sum H z, dz = g H, dw_post = sum dz v, db_post = sum dz,
+//   dy = r_y (dz w_post - k1 - v k2), k1 and k2 the same means over dz w_post
+// (sums over the rows that share the vector, means over the channels).
+#include "oc_device.h"
+#include "oc_launch.h"
+#include "oc_ops.h"
+#include <algorithm>
+
+namespace oc {
+
+namespace {
+
+constexpr int NORM_RMS = 1, NORM_LAYER = 2;   // oc_norm_kind
+
+// Eight consecutive elements as fp32, and back (rounded to nearest even; a NaN
+// stays one).
+__device__ __forceinline__ void load8(const uint16_t *p, float (&v)[8]) {
+    const uint4 w = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(u[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
+    *reinterpret_cast<f32x4 *>(v) = *reinterpret_cast<const f32x4 *>(p);
+    *reinterpret_cast<f32x4 *>(v + 4) = *reinterpret_cast<const f32x4 *>(p + 4);
+}
+__device__ __forceinline__ void store8(uint16_t *p, const float (&v)[8]) {
+    bf16x8 o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
+    *reinterpret_cast<bf16x8 *>(p) = o;
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
+    *reinterpret_cast<f32x4 *>(p) = *reinterpret_cast<const f32x4 *>(v);
+    *reinterpret_cast<f32x4 *>(p + 4) = *reinterpret_cast<const f32x4 *>(v + 4);
+}
+template <typename T>
+__device__ __forceinline__ void load8_or(const T *p, long at, float other, float (&v)[8]) {
+    if (p != nullptr) {
+        load8(p + at, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = other;
+    }
+}
+
+// Sum over the block's 256 threads, the same order for every thread.
+__device__ __forceinline__ float block_sum(float v, float *red) {
+    v = wave_sum(v);
+    __syncthreads();   // red may still be read
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+struct Stats { float mean, rstd; };
+
+// One row, its chunks of 8 channels spread over the block.
+template <typename T>
+struct NormRow {
+    const NormArgs &a;
+    long at, mod;
+    Stats sy, sh;
+    __device__ __forceinline__ NormRow(const NormArgs &args, long row)
+        : a(args), at(row * args.C), mod(row / args.rows_per_mod * args.ld), sy{0.f, 1.f}, sh{0.f, 1.f} {}
+    // v = (y - mean) rstd and z
+    __device__ __forceinline__ void post(int c, float (&v)[8], float (&z)[8]) const {
+        float w[8], b[8];
+        load8((const T *)a.y + at + c, v);
+        load8_or((const T *)a.post_w, c, 1.f, w);
+        load8_or((const T *)a.post_b, c, 0.f, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = (v[i] - sy.mean) * sy.rstd;
+            z[i] = fmaf(v[i], w[i], b[i]);
+        }
+    }
+    __device__ __forceinline__ void stream(int c, float (&h)[8]) const {
+        load8((const T *)a.x + at + c, h);
+        if (a.y == nullptr) return;
+        float v[8], z[8], g[8];
+        post(c, v, z);
+        load8_or((const T *)a.gate, mod + c, 1.f, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = fmaf(g[i], z[i], a.res_scale * h[i]);
+    }
+    // mean and 1/deviation of f(c, values) over the row
+    template <typename F>
+    __device__ __forceinline__ Stats stats(int kind, float eps, float *red, F f) const {
+        Stats s{0.f, 1.f};
+        if (kind == 0) return s;
+        float v[8], sum = 0.f;
+        if (kind == NORM_LAYER) {
+            for (int c = threadIdx.x * 8; c < a.C; c += 2048) {
+                f(c, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += v[i];
+            }
+            s.mean = block_sum(sum, red) / (float)a.C;
+            sum = 0.f;
+        }
+        for (int c = threadIdx.x * 8; c < a.C; c += 2048) {
+            f(c, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(v[i] - s.mean, v[i] - s.mean, sum);
+        }
+        s.rstd = 1.f / sqrtf(block_sum(sum, red) / (float)a.C + eps);
+        return s;
+    }
+    __device__ __forceinline__ void both_stats(float *red) {
+        if (a.y != nullptr)
+            sy = stats(a.post, a.post_eps, red, [&](int c, float (&v)[8]) { load8((const T *)a.y + at + c, v); });
+        sh = stats(a.pre, a.pre_eps, red, [&](int c, float (&v)[8]) { stream(c, v); });
+    }
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_norm_gate(NormArgs a, T *h, T *n) {
+    __shared__ float red[4];
+    const long row = folded_block();
+    if (row >= a.rows) return;
+    NormRow<T> r(a, row);
+    r.both_stats(red);
+    for (int c = threadIdx.x * 8; c < a.C; c += 2048) {
+        float v[8];
+        r.stream(c, v);
+        if (h != nullptr) store8(h + r.at + c, v);
+        if (n == nullptr) continue;
+        float w[8], b[8], s[8], t[8];
+        load8_or((const T *)a.pre_w, c, 1.f, w);
+        load8_or((const T *)a.pre_b, c, 0.f, b);
+        load8_or((const T *)a.scale, r.mod + c, 0.f, s);
+        load8_or((const T *)a.shift, r.mod + c, 0.f, t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float m = fmaf((v[i] - r.sh.mean) * r.sh.rstd, w[i], b[i]);
+            v[i] = fmaf(m, 1.f + s[i], t[i]);
+        }
+        store8(n + r.at + c, v);
+    }
+}
+
+// Statistics of a row that the column sums need again.
+struct RowStats { Stats sy, sh; float m1, m2; };
+
+// The gradient of a row's stream, element by element, once its means are known.
+template <typename T>
+struct GradRow : NormRow<T> {
+    using NormRow<T>::a;
+    using NormRow<T>::at;
+    using NormRow<T>::mod;
+    using NormRow<T>::sh;
+    const T *dh, *dn;
+    float m1 = 0.f, m2 = 0.f;
+    __device__ __forceinline__ GradRow(const NormArgs &args, long row, const T *dh_, const T *dn_)
+        : NormRow<T>(args, row), dh(dh_), dn(dn_) {}
+    // u, the weighted u, and da
+    __device__ __forceinline__ void inner(int c, float (&u)[8], float (&av)[8], float (&da)[8]) const {
+        float w[8], b[8], s[8];
+        this->stream(c, u);
+        load8_or((const T *)a.pre_w, c, 1.f, w);
+        load8_or((const T *)a.pre_b, c, 0.f, b);
+        load8_or((const T *)a.scale, mod + c, 0.f, s);
+        load8_or(dn, at + c, 0.f, da);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            u[i] = (u[i] - sh.mean) * sh.rstd;
+            av[i] = fmaf(u[i], w[i], b[i]);
+            da[i] *= 1.f + s[i];
+        }
+    }
+    __device__ __forceinline__ void stream_grad(int c, float (&H)[8]) const {
+        float u[8], av[8], da[8], w[8];
+        inner(c, u, av, da);
+        load8_or((const T *)a.pre_w, c, 1.f, w);
+        load8_or(dh, at + c, 0.f, H);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) H[i] = fmaf(sh.rstd, fmaf(da[i], w[i], -m1) - u[i] * m2, H[i]);
+    }
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_norm_grad_rows(NormArgs a, const T *dh, const T *dn, T *dx, T *dy,
+                                                        RowStats *rows) {
+    __shared__ float red[4];
+    const long row = folded_block();
+    if (row >= a.rows) return;
+    GradRow<T> r(a, row, dh, dn);
+    r.both_stats(red);
+    if (a.pre != 0 && dn != nullptr) {
+        float s1 = 0.f, s2 = 0.f;
+        for (int c = threadIdx.x * 8; c < a.C; c += 2048) {
+            float u[8], av[8], da[8], w[8];
+            r.inner(c, u, av, da);
+            load8_or((const T *)a.pre_w, c, 1.f, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s1 = fmaf(da[i], w[i], s1);
+                s2 = fmaf(da[i] * w[i], u[i], s2);
+            }
+        }
+        if (a.pre == NORM_LAYER) r.m1 = block_sum(s1, red) / (float)a.C;
+        r.m2 = block_sum(s2, red) / (float)a.C;
+    }
+    if (threadIdx.x == 0) rows[row] = RowStats{r.sy, r.sh, r.m1, r.m2};
+    // dz w_post, the gradient of the normalised y
+    auto inner_y = [&](int c, float (&H)[8], float (&v)[8], float (&d)[8]) {
+        float z[8], g[8], w[8];
+        r.stream_grad(c, H);
+        r.post(c, v, z);
+        load8_or((const T *)a.gate, r.mod + c, 1.f, g);
+        load8_or((const T *)a.post_w, c, 1.f, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = H[i] * g[i] * w[i];
+    };
+    float k1 = 0.f, k2 = 0.f, H[8], v[8], d[8];
+    if (dy != nullptr && a.post != 0) {
+        float s1 = 0.f, s2 = 0.f;
+        for (int c = threadIdx.x * 8; c < a.C; c += 2048) {
+            inner_y(c, H, v, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s1 += d[i];
+                s2 = fmaf(d[i], v[i], s2);
+            }
+        }
+        if (a.post == NORM_LAYER) k1 = block_sum(s1, red) / (float)a.C;
+        k2 = block_sum(s2, red) / (float)a.C;
+    }
+    for (int c = threadIdx.x * 8; c < a.C; c += 2048) {
+        if (dy != nullptr) {
+            inner_y(c, H, v, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = r.sy.rstd * (d[i] - k1 - v[i] * k2);
+            store8(dy + r.at + c, d);
+        } else {
+            r.stream_grad(c, H);
+        }
+        if (dx == nullptr) continue;
+        if (a.y != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) H[i] *= a.res_scale;
+        }
+        store8(dx + r.at + c, H);
+    }
+}
+
+// The vectors' gradients.  Part p sums `part` rows; a part's modulation sums go
+// out at every change of the modulation row: straight to the result where the
+// part holds all of its rows, else to one of two slots of the part (0: a
+// modulation row that an earlier part began, 1: one that this part begins).
+enum { Q_GATE, Q_SCALE, Q_SHIFT, Q_POSTW, Q_POSTB, Q_PREW, Q_PREB, N_Q };
+struct ColOut {
+    float *out[N_Q];        // results, or NULL
+    float *slots;           // [3][n_parts][2][C]
+    float *sums;            // [4][n_parts][C]
+    int part, n_parts;
+};
+
+template <typename T>
+__global__ __launch_bounds__(64) void k_norm_grad_cols(NormArgs a, const T *dh, const T *dn, const RowStats *rows,
+                                                       ColOut o) {
+    const int c = (blockIdx.y * 64 + threadIdx.x) * 8, p = blockIdx.x;
+    if (c >= a.C) return;
+    const long r0 = (long)p * o.part, r1 = min(r0 + o.part, (long)a.rows);
+    float q[N_Q][8] = {};
+    for (long row = r0; row < r1; ++row) {
+        GradRow<T> r(a, row, dh, dn);
+        const RowStats st = rows[row];
+        r.sy = st.sy;
+        r.sh = st.sh;
+        r.m1 = st.m1;
+        r.m2 = st.m2;
+        float u[8], av[8], da[8], d[8];
+        r.inner(c, u, av, da);
+        load8_or(dn, r.at + c, 0.f, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            q[Q_SCALE][i] = fmaf(d[i], av[i], q[Q_SCALE][i]);
+            q[Q_SHIFT][i] += d[i];
+            q[Q_PREW][i] = fmaf(da[i], u[i], q[Q_PREW][i]);
+            q[Q_PREB][i] += da[i];
+        }
+        if (a.y != nullptr) {
+            float H[8], v[8], z[8], g[8];
+            r.stream_grad(c, H);
+            r.post(c, v, z);
+            load8_or((const T *)a.gate, r.mod + c, 1.f, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                q[Q_GATE][i] = fmaf(H[i], z[i], q[Q_GATE][i]);
+                q[Q_POSTW][i] = fmaf(H[i] * g[i], v[i], q[Q_POSTW][i]);
+                q[Q_POSTB][i] = fmaf(H[i], g[i], q[Q_POSTB][i]);
+            }
+        }
+        const long m = row / a.rows_per_mod, begin = m * a.rows_per_mod;
+        const long end = min(begin + a.rows_per_mod, (long)a.rows);
+        if (row + 1 == end || row + 1 == r1) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                if (o.out[k] == nullptr) continue;
+                float *to = begin >= r0 && end <= r1
+                                ? o.out[k] + m * a.C
+                                : o.slots + (((long)k * o.n_parts + p) * 2 + (begin >= r0 ? 1 : 0)) * a.C;
+                store8(to + c, q[k]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) q[k][i] = 0.f;
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 3; k < N_Q; ++k)
+        if (o.out[k] != nullptr) store8(o.sums + ((long)(k - 3) * o.n_parts + p) * a.C + c, q[k]);
+}
+
+// Joins the parts, in their order: block p > 0 the modulation row that is the
+// first to cross the start of part p, block 0 the vectors of all rows.
+__global__ __launch_bounds__(64) void k_norm_grad_join(int C, int rows, int rows_per_mod, ColOut o) {
+    const int c = blockIdx.y * 64 + threadIdx.x, k = blockIdx.z;
+    if (c >= C || o.out[k] == nullptr || (k < 3) != (blockIdx.x > 0)) return;
+    float s = 0.f;
+    long m = 0;
+    if (k < 3) {
+        const long edge = (long)blockIdx.x * o.part, begin = edge / rows_per_mod * rows_per_mod;
+        if (begin == edge || begin < edge - o.part) return;   // none crosses, or an earlier block joins it
+        m = begin / rows_per_mod;
+        const long end = min(begin + rows_per_mod, (long)rows);
+        for (long p = blockIdx.x - 1; p <= (end - 1) / o.part; ++p)
+            s += o.slots[(((long)k * o.n_parts + p) * 2 + (p * o.part <= begin ? 1 : 0)) * C + c];
+    } else {
+        for (long p = 0; p < o.n_parts; ++p) s += o.sums[((long)(k - 3) * o.n_parts + p) * C + c];
+    }
+    o.out[k][m * C + c] = s;
+}
+
+__global__ void k_zero(float *p, int n) {
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) p[i] = 0.f;
+}
+
+size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+int norm_part(int rows) { return std::max(1, cdiv(rows, 1024)); }
+
+}  // namespace
+
+hipError_t launch_zero(float *p, int n, hipStream_t st) {
+    launch_k(k_zero, std::min(cdiv(n, 256), 1024), 256, 0, st, p, n);
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_gate(const NormArgs &a, void *h, void *n, hipStream_t st) {
+    StageScope _stage(st, "norm_gate");
+    const dim3 grid = folded_grid(a.rows, 256);
+    if (a.bf16) launch_k(k_norm_gate<uint16_t>, grid, 256, 0, st, a, (uint16_t *)h, (uint16_t *)n);
+    else launch_k(k_norm_gate<float>, grid, 256, 0, st, a, (float *)h, (float *)n);
+    return hipGetLastError();
+}
+
+size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod) {
+    if (rows <= 0) return 0;
+    const size_t parts = (size_t)cdiv(rows, norm_part(rows));
+    return up256((size_t)rows * sizeof(RowStats)) + up256((rows_per_mod > 0 ? 6 : 0) * parts * C * 4) +
+           up256(4 * parts * C * 4);
+}
+
+hipError_t launch_norm_gate_grad(const NormArgs &a, const void *dh, const void *dn, void *dx, void *dy,
+                                 const NormGrads &g, void *ws, hipStream_t st) {
+    StageScope _stage(st, "norm_gate_grad");
+    RowStats *rows = (RowStats *)ws;
+    ColOut o{{g.gate, g.scale, g.shift, g.post_w, g.post_b, g.pre_w, g.pre_b}, nullptr, nullptr, 0, 0};
+    o.part = norm_part(a.rows);
+    o.n_parts = cdiv(a.rows, o.part);
+    const bool mods = g.gate || g.scale || g.shift, vecs = g.post_w || g.post_b || g.pre_w || g.pre_b;
+    char *w = (char *)ws + up256((size_t)a.rows * sizeof(RowStats));
+    o.slots = (float *)w;
+    o.sums = (float *)(w + up256((mods ? 6 : 0) * (size_t)o.n_parts * a.C * 4));
+    const dim3 grid = folded_grid(a.rows, 256);
+    if (a.bf16)
+        launch_k(k_norm_grad_rows<uint16_t>, grid, 256, 0, st, a, (const uint16_t *)dh, (const uint16_t *)dn,
+                 (uint16_t *)dx, (uint16_t *)dy, rows);
+    else
+        launch_k(k_norm_grad_rows<float>, grid, 256, 0, st, a, (const float *)dh, (const float *)dn, (float *)dx,
+                 (float *)dy, rows);
+    if (!mods && !vecs) return hipGetLastError();
+    const dim3 cgrid((unsigned)o.n_parts, (unsigned)cdiv(a.C, 512));
+    if (a.bf16)
+        launch_k(k_norm_grad_cols<uint16_t>, cgrid, 64, 0, st, a, (const uint16_t *)dh, (const uint16_t *)dn, rows, o);
+    else
+        launch_k(k_norm_grad_cols<float>, cgrid, 64, 0, st, a, (const float *)dh, (const float *)dn, rows, o);
+    launch_k(k_norm_grad_join, dim3((unsigned)o.n_parts, (unsigned)cdiv(a.C, 64), N_Q), 64, 0, st, a.C, a.rows,
+             a.rows_per_mod, o);
+    return hipGetLastError();
+}
+
+}  // namespace oc

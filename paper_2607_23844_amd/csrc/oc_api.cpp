@@ -2,6 +2,7 @@
 // carving and launch sequencing.  No device memory is allocated here; all
 // work goes on the caller's stream.
 #include "../../include/oc.h"
+#include "oc_host.h"
 #include "oc_internal.h"
 
 #include <cmath>
@@ -435,6 +436,21 @@ namespace oc {
 oc_status record_error(oc_status s, const char *msg) {
     if (s == OC_OK) return ok();
     return fail(s, "%s", msg);
+}
+
+oc_status failf(oc_status s, const char *fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof(buf), fmt, ap);
+    va_end(ap);
+    return fail(s, "%s", buf);
+}
+
+oc_status valid_shape(const oc_shape *sh) { return check_shape(sh); }
+
+oc_status valid_ws(const void *ws, size_t ws_bytes, size_t need) {
+    return check_ws(const_cast<void *>(ws), ws_bytes, need);
 }
 }  // namespace oc
 

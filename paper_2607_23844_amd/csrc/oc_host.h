@@ -1,0 +1,23 @@
+// Host-side checks shared by the C-ABI sources: the thread's error message and
+// the checks that every entry point makes.
+#pragma once
+#include "../../include/oc.h"
+#include <cstddef>
+#include <cstdint>
+
+namespace oc {
+
+oc_status record_error(oc_status s, const char *msg);
+oc_status failf(oc_status s, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+oc_status valid_shape(const oc_shape *sh);
+oc_status valid_ws(const void *ws, size_t ws_bytes, size_t need);
+
+inline bool is_aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+// [a, a + na) and [b, b + nb) share a byte (NULL shares none)
+inline bool overlaps(const void *a, size_t na, const void *b, size_t nb) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && na && nb && x < y + nb && y < x + na;
+}
+
+}  // namespace oc

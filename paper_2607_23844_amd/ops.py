@@ -1,0 +1,195 @@
+"""The operators around a sublayer, with the names of the C ABI (include/oc.h):
+norms fused with gate, modulation and residual, and their gradients.
+
+As in api.py this is argument marshalling only.  Tensors are on one GPU, which
+need not be the current one; the work goes on that GPU's current stream.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+from dataclasses import dataclass
+from typing import Dict, Optional, Sequence
+
+import torch
+
+from . import _lib as L
+from .api import Shape, _ptr
+
+
+@dataclass
+class Norm:
+    """A norm over the channels, then weights and biases (None: 1 and 0)."""
+    kind: str = "layer"      # none | rms | layer
+    eps: float = 1e-6
+    w: Optional[torch.Tensor] = None
+    b: Optional[torch.Tensor] = None
+
+
+@dataclass
+class Mod:
+    """Modulation vectors [n_mod, C], which may be columns of one wider
+    product; rows_per_mod consecutive rows share one (None: all rows)."""
+    gate: Optional[torch.Tensor] = None
+    scale: Optional[torch.Tensor] = None
+    shift: Optional[torch.Tensor] = None
+    rows_per_mod: Optional[int] = None
+
+
+_SAME = contextlib.nullcontext()
+
+
+def _on(t: torch.Tensor):
+    """The tensor's GPU as the current one for the call's launches."""
+    return _SAME if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
+def _stream_of(t: torch.Tensor) -> int:
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _bad(status: int, message: str):
+    return L.OmniCacheError(status, message)
+
+
+def _gpu(t, name: str) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise _bad(L.OC_ERR_INVALID_ARG, f"{name} must be a GPU tensor")
+    return t
+
+
+def _like(t: Optional[torch.Tensor], shape, dtype, dev, name: str) -> Optional[int]:
+    """The address of a contiguous tensor of this shape, type and GPU (None: NULL)."""
+    if t is None:
+        return None
+    if _gpu(t, name).dtype != dtype:
+        raise _bad(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.device != dev:
+        raise _bad(L.OC_ERR_INVALID_ARG, f"{name} is on {t.device}, expected {dev}")
+    if t.shape != shape:
+        raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise _bad(L.OC_ERR_INVALID_ARG, f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _norm(n: Optional[Norm], shape: Shape, dev, name: str) -> Optional[L.oc_norm]:
+    if n is None:
+        return None
+    if n.kind not in L.NORMS:
+        raise _bad(L.OC_ERR_INVALID_ARG, f"{name}: unknown norm {n.kind!r}")
+    c, dt = (shape.C,), shape.torch_dtype
+    return L.oc_norm(L.NORMS[n.kind], n.eps, _like(n.w, c, dt, dev, name + ".w"), _like(n.b, c, dt, dev, name + ".b"))
+
+
+def _mod(m: Optional[Mod], rows: int, shape: Shape, dev) -> Optional[L.oc_mod]:
+    if m is None:
+        return None
+    per = max(rows, 1) if m.rows_per_mod is None else m.rows_per_mod
+    if per < 1:
+        raise _bad(L.OC_ERR_INVALID_ARG, f"rows_per_mod={per} must be >= 1")
+    n_mod, ld, at = -(-rows // per), None, []
+    for name, t in (("gate", m.gate), ("scale", m.scale), ("shift", m.shift)):
+        if t is None:
+            at.append(None)
+            continue
+        if _gpu(t, name).dtype != shape.torch_dtype:
+            raise _bad(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected {shape.torch_dtype}")
+        if t.device != dev:
+            raise _bad(L.OC_ERR_INVALID_ARG, f"{name} is on {t.device}, expected {dev}")
+        if t.dim() == 1:
+            t = t[None]
+        if t.shape != (n_mod, shape.C):
+            raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(t.shape)}, expected {(n_mod, shape.C)}")
+        if t.stride(1) != 1 and shape.C > 1:
+            raise _bad(L.OC_ERR_INVALID_ARG, f"the channels of {name} must be contiguous")
+        row = t.stride(0) if n_mod > 1 else shape.C
+        if ld is not None and row != ld:
+            raise _bad(L.OC_ERR_INVALID_ARG, "gate, scale and shift must have the same row stride")
+        ld = row
+        at.append(t.data_ptr())
+    return L.oc_mod(*at, shape.C if ld is None else ld, per, 0)
+
+
+def _rows_of(x: torch.Tensor, shape: Shape) -> int:
+    if _gpu(x, "x").dim() < 1 or x.shape[-1] != shape.C:
+        raise _bad(L.OC_ERR_SHAPE, f"x has shape {tuple(x.shape)}, expected [..., {shape.C}]")
+    return x.numel() // shape.C
+
+
+def _ref(s):
+    return None if s is None else C.byref(s)
+
+
+def norm_gate(x: torch.Tensor, shape: Shape, y: Optional[torch.Tensor] = None, post: Optional[Norm] = None,
+              pre: Optional[Norm] = None, mod: Optional[Mod] = None, res_scale: float = 1.0, h=None, n=None):
+    """oc_norm_gate: h = res_scale x + gate post(y) and n = pre(h)(1 + scale) +
+    shift over the last dimension.  h and n: a tensor to write (x or y
+    themselves are possible), None (a new one) or False (not wanted).  Without
+    y, h is x.  Returns (h, n)."""
+    rows = _rows_of(x, shape)
+    dev, dt, full = x.device, shape.torch_dtype, x.shape
+    xp, yp = _like(x, full, dt, dev, "x"), _like(y, full, dt, dev, "y")
+    if y is None:
+        if h is not None and h is not False:
+            raise _bad(L.OC_ERR_INVALID_ARG, "h is x where y is None")
+        h = False
+    h = torch.empty_like(x) if h is None else h
+    n = torch.empty_like(x) if n is None else n
+    hp = None if h is False else _like(h, full, dt, dev, "h")
+    np_ = None if n is False else _like(n, full, dt, dev, "n")
+    sh, po, pr, mo = shape.c(), _norm(post, shape, dev, "post"), _norm(pre, shape, dev, "pre"), _mod(mod, rows, shape, dev)
+    if rows == 0:      # (empty tensors have no address)
+        hp = np_ = xp = yp = None
+    with _on(x):
+        L.check(L.lib().oc_norm_gate(C.byref(sh), rows, xp, yp, _ref(po), _ref(pr), _ref(mo), res_scale, hp, np_,
+                                     _stream_of(x)))
+    return (x if y is None else None if h is False else h), (None if n is False else n)
+
+
+def norm_gate_grad_workspace_bytes(shape: Shape, rows: int, rows_per_mod: int = 0) -> int:
+    sh = shape.c()
+    return int(L.lib().oc_norm_gate_grad_workspace_bytes(C.byref(sh), rows, rows_per_mod))
+
+
+def norm_gate_grad(x: torch.Tensor, shape: Shape, dn: Optional[torch.Tensor] = None,
+                   dh: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, post: Optional[Norm] = None,
+                   pre: Optional[Norm] = None, mod: Optional[Mod] = None, res_scale: float = 1.0,
+                   want: Optional[Sequence[str]] = None,
+                   ws: Optional[torch.Tensor] = None) -> Dict[str, Optional[torch.Tensor]]:
+    """oc_norm_gate_grad: the gradients of norm_gate's inputs from those of its
+    outputs (None: zero), as a dict with dx, dy (like x) and, in fp32, gate,
+    scale, shift [n_mod, C], post_w, post_b, pre_w, pre_b [C]; None for what
+    the call has not, or what `want` (None: everything) leaves out."""
+    rows = _rows_of(x, shape)
+    dev, dt, full = x.device, shape.torch_dtype, x.shape
+    xp, yp = _like(x, full, dt, dev, "x"), _like(y, full, dt, dev, "y")
+    dnp, dhp = _like(dn, full, dt, dev, "dn"), _like(dh, full, dt, dev, "dh")
+    sh, po, pr, mo = shape.c(), _norm(post, shape, dev, "post"), _norm(pre, shape, dev, "pre"), _mod(mod, rows, shape, dev)
+    per = mo.rows_per_mod if mo is not None else 0
+    n_mod = -(-rows // per) if per else 0
+    has = {"dx": True, "dy": y is not None}
+    has.update({k: getattr(mo, k) is not None if mo is not None else False for k in ("gate", "scale", "shift")})
+    for k, s in (("post", po), ("pre", pr)):
+        has.update({k + "_w": s is not None and s.w is not None, k + "_b": s is not None and s.b is not None})
+    if want is not None and not set(want) <= set(has):
+        raise _bad(L.OC_ERR_INVALID_ARG, f"unknown gradients {sorted(set(want) - set(has))}")
+    out = {}
+    for k, there in has.items():
+        if not there or (want is not None and k not in want):
+            out[k] = None
+        elif k in ("dx", "dy"):
+            out[k] = torch.empty_like(x)
+        else:
+            out[k] = torch.empty((n_mod, shape.C) if k in ("gate", "scale", "shift") else (shape.C,),
+                                 dtype=torch.float32, device=dev)
+    if ws is None:
+        ws = torch.empty(max(norm_gate_grad_workspace_bytes(shape, rows, per), 256), dtype=torch.uint8, device=dev)
+    elif _gpu(ws, "ws").device != dev or not ws.is_contiguous():
+        raise _bad(L.OC_ERR_INVALID_ARG, f"ws must be contiguous and on {dev}")
+    g = L.oc_norm_grads(*(_ptr(out[k]) for k in ("gate", "scale", "shift", "post_w", "post_b", "pre_w", "pre_b")))
+    with _on(x):
+        L.check(L.lib().oc_norm_gate_grad(C.byref(sh), rows, xp, yp, _ref(po), _ref(pr), _ref(mo), res_scale, dhp, dnp,
+                                          _ptr(out["dx"]), _ptr(out["dy"]), C.byref(g), ws.data_ptr(),
+                                          ws.numel() * ws.element_size(), _stream_of(x)))
+    return out

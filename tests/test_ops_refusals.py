@@ -1,0 +1,150 @@
+"""The operators around a sublayer refuse bad arguments on the host, before
+anything is enqueued, and the 64-bit formulas of their tests are consistent.
+No test here touches a GPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2607_23844_amd as oc
+from paper_2607_23844_amd import _lib as L
+from ops_ref import NormGate
+
+A = 1 << 30          # addresses that are never read: every call below is refused before a launch
+STEP = 1 << 24
+
+
+def at(i):
+    return A + i * STEP
+
+
+def test_struct_sizes():
+    assert C.sizeof(L.oc_norm) == 24 and C.sizeof(L.oc_mod) == 40 and C.sizeof(L.oc_norm_grads) == 56
+
+
+def norm_call(shape=None, rows=4, x=at(0), y=at(1), post=None, pre=None, mod=None, rs=1.0, h=at(2), n=at(3)):
+    sh = (shape or oc.Shape(1, 1, 1, 64, 1, 16, 0, "bf16")).c()
+    ref = [None if v is None else C.byref(v) for v in (post, pre, mod)]
+    return L.lib().oc_norm_gate(C.byref(sh), rows, x, y, *ref, rs, h, n, None)
+
+
+def mod(gate=at(4), scale=at(5), shift=at(6), ld=64, per=4, reserved=0):
+    return L.oc_mod(gate, scale, shift, ld, per, reserved)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(rows=-1), L.OC_ERR_SHAPE),
+    (dict(rows=1 << 30), L.OC_ERR_SHAPE),
+    (dict(shape=oc.Shape(1, 1, 1, 60, 1, 16, 0, "bf16")), L.OC_ERR_SHAPE),
+    (dict(x=None), L.OC_ERR_INVALID_ARG),
+    (dict(x=at(0) + 8), L.OC_ERR_INVALID_ARG),
+    (dict(y=at(1) + 2), L.OC_ERR_INVALID_ARG),
+    (dict(h=at(2) + 4), L.OC_ERR_INVALID_ARG),
+    (dict(n=at(3) + 4), L.OC_ERR_INVALID_ARG),
+    (dict(h=None, n=None), L.OC_ERR_INVALID_ARG),
+    (dict(y=None), L.OC_ERR_INVALID_ARG),                                       # h without y
+    (dict(y=None, h=None, rs=0.5), L.OC_ERR_INVALID_ARG),
+    (dict(y=None, h=None, post=L.oc_norm(1, 1e-6, None, None)), L.OC_ERR_INVALID_ARG),
+    (dict(y=None, h=None, mod=mod()), L.OC_ERR_INVALID_ARG),                     # a gate without y
+    (dict(rs=float("nan")), L.OC_ERR_INVALID_ARG),
+    (dict(rs=float("inf")), L.OC_ERR_INVALID_ARG),
+    (dict(pre=L.oc_norm(3, 1e-6, None, None)), L.OC_ERR_INVALID_ARG),
+    (dict(pre=L.oc_norm(-1, 1e-6, None, None)), L.OC_ERR_INVALID_ARG),
+    (dict(pre=L.oc_norm(1, -1e-6, None, None)), L.OC_ERR_INVALID_ARG),
+    (dict(pre=L.oc_norm(1, float("nan"), None, None)), L.OC_ERR_INVALID_ARG),
+    (dict(post=L.oc_norm(1, float("inf"), None, None)), L.OC_ERR_INVALID_ARG),
+    (dict(pre=L.oc_norm(1, 1e-6, at(7) + 8, None)), L.OC_ERR_INVALID_ARG),
+    (dict(mod=mod(ld=56)), L.OC_ERR_SHAPE),
+    (dict(mod=mod(ld=68)), L.OC_ERR_SHAPE),
+    (dict(mod=mod(per=0)), L.OC_ERR_INVALID_ARG),
+    (dict(mod=mod(per=-4)), L.OC_ERR_INVALID_ARG),
+    (dict(mod=mod(reserved=1)), L.OC_ERR_INVALID_ARG),
+    (dict(mod=mod(gate=at(4) + 2)), L.OC_ERR_INVALID_ARG),
+    (dict(h=at(0) + 64), L.OC_ERR_INVALID_ARG),                                  # overlaps x without being it
+    (dict(n=at(1) - 64), L.OC_ERR_INVALID_ARG),
+    (dict(n=at(2)), L.OC_ERR_INVALID_ARG),                                       # h and n the same
+    (dict(h=at(5), mod=mod()), L.OC_ERR_INVALID_ARG),
+    (dict(n=at(7), pre=L.oc_norm(1, 1e-6, at(7), None)), L.OC_ERR_INVALID_ARG),
+])
+def test_norm_gate_refuses(kw, status):
+    assert norm_call(**kw) == status
+    assert L.lib().oc_last_error() != b""
+
+
+def grad_call(shape=None, rows=4, x=at(0), y=at(1), post=None, pre=None, m=None, dh=at(2), dn=at(3), dx=at(4),
+              dy=at(5), grads=None, ws=at(9), ws_bytes=None, rs=1.0):
+    sh = (shape or oc.Shape(1, 1, 1, 64, 1, 16, 0, "bf16")).c()
+    need = L.lib().oc_norm_gate_grad_workspace_bytes(C.byref(sh), rows, m.rows_per_mod if m else 0)
+    ref = [None if v is None else C.byref(v) for v in (post, pre, m)]
+    g = None if grads is None else C.byref(grads)
+    return L.lib().oc_norm_gate_grad(C.byref(sh), rows, x, y, *ref, rs, dh, dn, dx, dy, g, ws,
+                                     need if ws_bytes is None else ws_bytes, None)
+
+
+def grads(**kw):
+    return L.oc_norm_grads(*(kw.get(k) for k, _ in L.oc_norm_grads._fields_))
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dh=None, dn=None), L.OC_ERR_INVALID_ARG),
+    (dict(y=None), L.OC_ERR_INVALID_ARG),                                        # dy without y
+    (dict(grads=grads(gate=at(6))), L.OC_ERR_INVALID_ARG),                       # no gate
+    (dict(grads=grads(pre_w=at(6)), pre=L.oc_norm(1, 1e-6, None, None)), L.OC_ERR_INVALID_ARG),
+    (dict(grads=grads(post_b=at(6)), post=L.oc_norm(1, 1e-6, at(7), None)), L.OC_ERR_INVALID_ARG),
+    (dict(grads=grads(pre_w=at(6) + 4), pre=L.oc_norm(1, 1e-6, at(7), None)), L.OC_ERR_INVALID_ARG),
+    (dict(ws_bytes=1), L.OC_ERR_WORKSPACE),
+    (dict(ws=None), L.OC_ERR_INVALID_ARG),
+    (dict(ws=at(9) + 16), L.OC_ERR_INVALID_ARG),
+    (dict(dx=at(0)), L.OC_ERR_INVALID_ARG),
+    (dict(dx=at(2)), L.OC_ERR_INVALID_ARG),
+    (dict(dy=at(4)), L.OC_ERR_INVALID_ARG),
+    (dict(dy=at(9)), L.OC_ERR_INVALID_ARG),
+    (dict(dh=at(2) + 2), L.OC_ERR_INVALID_ARG),
+    (dict(grads=grads(pre_w=at(4)), pre=L.oc_norm(1, 1e-6, at(7), None)), L.OC_ERR_INVALID_ARG),
+    (dict(grads=grads(pre_w=at(7)), pre=L.oc_norm(1, 1e-6, at(7), None)), L.OC_ERR_INVALID_ARG),
+    (dict(rows=-2, ws_bytes=1 << 20), L.OC_ERR_SHAPE),
+])
+def test_norm_gate_grad_refuses(kw, status):
+    assert grad_call(**kw) == status
+
+
+def test_gradient_workspace_covers_its_parts():
+    f = L.lib().oc_norm_gate_grad_workspace_bytes
+    sh = oc.Shape(1, 1, 1, 64, 1, 16, 0, "bf16").c()
+    assert f(C.byref(sh), 0, 0) == 0 and f(C.byref(sh), -1, 0) == 0 and f(C.byref(sh), 4, -1) == 0
+    assert f(C.byref(sh), 1000, 1) >= f(C.byref(sh), 1000, 0) > 0
+
+
+def test_python_wrappers_refuse_host_tensors():
+    sh = oc.Shape(1, 1, 1, 64, 1, 16, 0, "f32")
+    with pytest.raises(oc.OmniCacheError):
+        oc.norm_gate(torch.zeros(2, 64), sh)
+    with pytest.raises(oc.OmniCacheError):
+        oc.norm_gate_grad(torch.zeros(2, 64), sh, dn=torch.zeros(2, 64))
+
+
+@pytest.mark.parametrize("pre,post", [("layer", "rms"), ("rms", "layer"), ("none", "layer"), ("layer", "none")])
+def test_norm_formulas_against_differences(pre, post):
+    g = torch.Generator().manual_seed(3)
+
+    def r(*s):
+        return torch.randn(*s, generator=g, dtype=torch.float64)
+
+    rows, ch, per = 5, 16, 2
+    t = dict(x=r(rows, ch), y=r(rows, ch), gate=r(3, ch), scale=r(3, ch), shift=r(3, ch), post_w=r(ch), post_b=r(ch),
+             pre_w=r(ch), pre_b=r(ch))
+    dh, dn = r(rows, ch), r(rows, ch)
+
+    def make(v):
+        return NormGate(v["x"], v["y"], (post, 1e-3, v["post_w"], v["post_b"]), (pre, 1e-3, v["pre_w"], v["pre_b"]),
+                        v["gate"], v["scale"], v["shift"], per, 0.6)
+
+    got = make(t).grads(dh, dn)
+    for k in t:
+        by = r(*t[k].shape) * 1e-5
+        val = []
+        for s in (1, -1):
+            o = make({**t, k: t[k] + s * by})
+            val.append(float((o.h * dh + o.n * dn).sum()))
+        along = 2 * float((got["d" + k if k in "xy" else k][0].reshape(by.shape) * by).sum())
+        assert abs(val[0] - val[1] - along) <= 1e-6 * (abs(along) + 1e-5), k
