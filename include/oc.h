@@ -459,6 +459,79 @@ oc_status oc_attn_full(const oc_shape *shape, const oc_cfg *cfg, const void *x, 
                        void *ws, size_t ws_bytes, hipStream_t stream);
 
 /*
+ * Rotary positions with up to three axes (time, height, width): pairs of
+ * channels of every q and k head are turned by angles proportional to the
+ * token's position on the F x H x W grid, so that q.k depends on differences
+ * of positions.  Under a cache the retained tokens keep their own positions.
+ */
+typedef enum {
+    OC_ROPE_PAIRS = 0,        /* pair p: channels 2p and 2p + 1                                  */
+    OC_ROPE_HALVES = 1,       /* an axis' channels in two halves: pair i of an axis whose d
+                                 channels start at o is (o + i, o + i + d/2)                     */
+    OC_ROPE_SPLIT = 2         /* all rotated channels in two halves: pair p of P is (p, p + P)   */
+} oc_rope_layout;
+
+typedef struct {
+    int32_t dim[3];           /* channels of a head turned by time, height and width, in this
+                                 order from channel 0: even, >= 0, in all 2P with
+                                 2 <= 2P <= head_dim; channels from 2P on are not turned         */
+    int32_t layout;           /* oc_rope_layout                                                  */
+    int32_t shared;           /* 0: pair i of an axis with d channels has frequency
+                                 theta^(-2 i / d); 1: one spectrum for all axes, pair p
+                                 (counted over the axes) has theta^(-p / P)                      */
+    int32_t origin[3];        /* position of frame 0, image row 0, image column 0                */
+    double  theta;            /* finite, > 0                                                     */
+    double  scale[3];         /* finite: positions are multiplied by it                          */
+} oc_rope;
+
+/*
+ * oc_rope_qk — turns n_rows rows of q (shape->heads heads) and k (k_heads
+ * heads of the same width; q or k may be NULL): (a, b) of a pair becomes
+ * (a cos - b sin, a sin + b cos) with angle = (position + origin) * scale *
+ * frequency, or minus that angle when inverse is 1 (which is also the
+ * gradient: the inputs' gradients from the outputs').  The position of row r
+ * is that of token t = kept_idx[r] (or r where kept_idx is NULL): frame t / N,
+ * image row (t mod N) / W, image column t mod W; or, with pos given (kept_idx
+ * NULL), pos[3r .. 3r+2].  Rows whose kept_idx lies outside [0, F*N) are left
+ * alone (not read, not written).  Row r of q starts at q + r * ld_q elements
+ * and holds its heads contiguously, so q and k may be columns of a projected
+ * buffer; the outputs likewise with ld_qo and ld_ko.  An output may be its
+ * input with the same row stride (in place) and overlaps nothing otherwise.
+ * Element type: shape's.  Angles are reduced in 64 bits, the rotation is fp32
+ * and rounded once; channels that are not turned are copied.
+ * Pointers 16-byte aligned, row strides multiples of 16 bytes and at least a
+ * row's width; without kept_idx and pos, n_rows <= F*N.
+ */
+oc_status oc_rope_qk(const oc_shape *shape, const oc_rope *rope, int32_t n_rows, const int32_t *kept_idx,
+                     const int32_t *pos, const void *q, int64_t ld_q, const void *k, int64_t ld_k, int32_t k_heads,
+                     void *q_out, int64_t ld_qo, void *k_out, int64_t ld_ko, int32_t inverse, hipStream_t stream);
+
+/*
+ * oc_attn_reduced_rope, oc_layer_cached_rope, oc_attn_full_rope — the calls
+ * without _rope, with the projected q and k turned by their tokens' positions
+ * before the attention (temporal layers: dim = {d, 0, 0}).  Context rows are
+ * not turned.  Matching, selection and restoration do not change.  rope NULL:
+ * exactly the call without it.  oc_attn_reduced_rope takes the tokens of its
+ * rows: kept_idx [n_seq * seq_len], as oc_gather got it (rows outside [0, F*N)
+ * are not turned).  bf16 layers hold q and k in fp16 before and after the
+ * rotation (a second rounding of 2^-11); head_dim 64 layers of short
+ * sequences give up the fused projection and attention for it.  Workspaces
+ * as without _rope.
+ */
+oc_status oc_attn_reduced_rope(const oc_shape *shape, const oc_rope *rope, const int32_t *kept_idx,
+                               const void *x_kept, int32_t n_seq, int32_t seq_len, const void *ctx,
+                               const oc_attn_weights *w, void *y_kept, void *y_ctx, void *ws, size_t ws_bytes,
+                               hipStream_t stream);
+
+oc_status oc_layer_cached_rope(const oc_shape *shape, const oc_cfg *cfg, const oc_rope *rope, const void *x,
+                               const void *ctx, const oc_attn_weights *w, oc_cache *cache, void *y_ctx,
+                               oc_trace *trace, void *ws, size_t ws_bytes, hipStream_t stream);
+
+oc_status oc_attn_full_rope(const oc_shape *shape, const oc_cfg *cfg, const oc_rope *rope, const void *x,
+                            const void *ctx, const oc_attn_weights *w, void *y, void *y_ctx, void *ws,
+                            size_t ws_bytes, hipStream_t stream);
+
+/*
  * Layered Cache schedule proposal (§3.4, Alg. 1), host only.  For each
  * candidate layer-timestep pair (l, t) the caller gives the latency L[l,t]
  * that reusing the cache there saves and the quality loss Q[l,t] it costs

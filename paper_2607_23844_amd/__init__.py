@@ -13,6 +13,7 @@ from .api import (  # noqa: F401
     Cfg,
     LayerCache,
     PlanInfo,
+    Rope,
     Shape,
     StageTimer,
     attn_full,
@@ -42,4 +43,5 @@ from .ops import (  # noqa: F401
     norm_gate,
     norm_gate_grad,
     norm_gate_grad_workspace_bytes,
+    rope_qk,
 )

@@ -12,6 +12,7 @@ OC_OK, OC_ERR_INVALID_ARG, OC_ERR_SHAPE, OC_ERR_DTYPE, OC_ERR_WORKSPACE, OC_ERR_
 OC_F32, OC_BF16 = 0, 1
 GRANS = {"token": 0, "frame": 1, "block": 2, "frame_token": 3}
 COLDS = {"matched": 0, "full": 1}
+ROPE_LAYOUTS = {"pairs": 0, "halves": 1, "split": 2}
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 
 
@@ -69,6 +70,11 @@ class oc_norm_grads(C.Structure):
                 ("post_b", C.c_void_p), ("pre_w", C.c_void_p), ("pre_b", C.c_void_p)]
 
 
+class oc_rope(C.Structure):
+    _fields_ = [("dim", C.c_int32 * 3), ("layout", C.c_int32), ("shared", C.c_int32), ("origin", C.c_int32 * 3),
+                ("theta", C.c_double), ("scale", C.c_double * 3)]
+
+
 class oc_cache_entry(C.Structure):
     _fields_ = [("layer", C.c_int32), ("step", C.c_int32), ("interval", C.c_int32)]
 
@@ -109,6 +115,17 @@ _SIGS = {
                                     P(oc_mod), C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                     P(oc_norm_grads), C.c_void_p, C.c_size_t, C.c_void_p]),
     "oc_norm_gate_grad_workspace_bytes": (C.c_size_t, [P(oc_shape), C.c_int32, C.c_int32]),
+    "oc_rope_qk": (C.c_int, [P(oc_shape), P(oc_rope), C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                             C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                             C.c_int32, C.c_void_p]),
+    "oc_attn_reduced_rope": (C.c_int, [P(oc_shape), P(oc_rope), C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+                                       C.c_void_p, P(oc_attn_weights), C.c_void_p, C.c_void_p, C.c_void_p,
+                                       C.c_size_t, C.c_void_p]),
+    "oc_layer_cached_rope": (C.c_int, [P(oc_shape), P(oc_cfg), P(oc_rope), C.c_void_p, C.c_void_p,
+                                       P(oc_attn_weights), P(oc_cache), C.c_void_p, P(oc_trace), C.c_void_p,
+                                       C.c_size_t, C.c_void_p]),
+    "oc_attn_full_rope": (C.c_int, [P(oc_shape), P(oc_cfg), P(oc_rope), C.c_void_p, C.c_void_p, P(oc_attn_weights),
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "oc_block_cached": (C.c_int, [P(oc_shape), P(oc_cfg), P(oc_cfg), C.c_void_p, P(oc_attn_weights),
                                   P(oc_attn_weights), P(oc_cache), P(oc_cache), C.c_void_p, P(oc_trace), P(oc_trace),
                                   C.c_void_p, C.c_size_t, C.c_void_p]),

@@ -55,6 +55,25 @@ class Cfg:
                         self.r_coarse)
 
 
+@dataclass(frozen=True)
+class Rope:
+    """Rotary positions: channels of a head turned by time, height and width."""
+    dims: Tuple[int, int, int]
+    theta: float = 10000.0
+    layout: str = "pairs"    # pairs | halves | split
+    shared: bool = False     # one spectrum over all axes
+    origin: Tuple[int, int, int] = (0, 0, 0)
+    scale: Tuple[float, float, float] = (1.0, 1.0, 1.0)
+
+    def c(self) -> L.oc_rope:
+        if len(self.dims) != 3 or len(self.origin) != 3 or len(self.scale) != 3:
+            raise L.OmniCacheError(L.OC_ERR_SHAPE, "dims, origin and scale have an entry for each of the three axes")
+        if self.layout not in L.ROPE_LAYOUTS:
+            raise L.OmniCacheError(L.OC_ERR_INVALID_ARG, f"unknown rotary layout {self.layout!r}")
+        return L.oc_rope((C.c_int32 * 3)(*self.dims), L.ROPE_LAYOUTS[self.layout], 1 if self.shared else 0,
+                         (C.c_int32 * 3)(*self.origin), self.theta, (C.c_double * 3)(*self.scale))
+
+
 @dataclass
 class PlanInfo:
     n_groups: int
@@ -97,6 +116,10 @@ def _need(t: torch.Tensor, dtype: torch.dtype, name: str) -> None:
         raise L.OmniCacheError(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected {dtype}")
     if not t.is_contiguous():
         raise L.OmniCacheError(L.OC_ERR_INVALID_ARG, f"{name} must be contiguous")
+
+
+def _rope(rope: Optional[Rope]):
+    return None if rope is None else C.byref(rope.c())
 
 
 def _weights(w: Dict[str, torch.Tensor], shape: Shape) -> L.oc_attn_weights:
@@ -180,8 +203,10 @@ def attn_workspace_bytes(shape: Shape, n_seq: int, seq_len: int) -> int:
 
 
 def attn_reduced(x_kept: torch.Tensor, n_seq: int, seq_len: int, weights: Dict[str, torch.Tensor], shape: Shape,
-                 ctx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
-    """(y_kept [n_seq*seq_len, C], y_ctx [n_ctx, C] or None)"""
+                 ctx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                 rope: Optional[Rope] = None, kept_idx: Optional[torch.Tensor] = None):
+    """(y_kept [n_seq*seq_len, C], y_ctx [n_ctx, C] or None).  rope: q and k
+    turned by the positions of the rows' tokens kept_idx."""
     _need(x_kept, shape.torch_dtype, "x_kept")
     w = _weights(weights, shape)
     dev = x_kept.device
@@ -193,9 +218,14 @@ def attn_reduced(x_kept: torch.Tensor, n_seq: int, seq_len: int, weights: Dict[s
     need = attn_workspace_bytes(shape, n_seq, seq_len)
     if ws is None:
         ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    if rope is not None:
+        _need(kept_idx, torch.int32, "kept_idx")
+        if kept_idx.numel() != n_seq * seq_len:
+            raise L.OmniCacheError(L.OC_ERR_SHAPE, f"kept_idx has {kept_idx.numel()} entries for {n_seq * seq_len} rows")
     sh = shape.c()
-    L.check(L.lib().oc_attn_reduced(C.byref(sh), x_kept.data_ptr(), n_seq, seq_len, _ptr(ctx), C.byref(w),
-                                    y.data_ptr(), _ptr(y_ctx), ws.data_ptr(), ws.numel(), _stream(x_kept)))
+    L.check(L.lib().oc_attn_reduced_rope(C.byref(sh), _rope(rope), _ptr(kept_idx), x_kept.data_ptr(), n_seq, seq_len,
+                                         _ptr(ctx), C.byref(w), y.data_ptr(), _ptr(y_ctx), ws.data_ptr(), ws.numel(),
+                                         _stream(x_kept)))
     return y[:n_seq * seq_len], y_ctx
 
 
@@ -252,15 +282,17 @@ def _layer_args(x, weights, cache, shape, cfg, ctx, trace):
 
 
 def layer_cached(x: torch.Tensor, weights: Dict[str, torch.Tensor], cache: LayerCache, shape: Shape, cfg: Cfg,
-                 ctx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, trace: bool = False):
-    """One cached layer call; returns (cache.y, y_ctx, trace dict or None)."""
+                 ctx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, trace: bool = False,
+                 rope: Optional[Rope] = None):
+    """One cached layer call; returns (cache.y, y_ctx, trace dict or None).
+    rope: q and k turned by the retained tokens' positions."""
     w, pl, y_ctx, tr, out, c = _layer_args(x, weights, cache, shape, cfg, ctx, trace)
     if ws is None:
         ws = workspace(shape, cfg, x.device)
     sh, cf = shape.c(), cfg.c()
-    L.check(L.lib().oc_layer_cached(C.byref(sh), C.byref(cf), x.data_ptr(), _ptr(ctx), C.byref(w), C.byref(c),
-                                    _ptr(y_ctx), C.byref(tr) if tr is not None else None, ws.data_ptr(), ws.numel(),
-                                    _stream(x)))
+    L.check(L.lib().oc_layer_cached_rope(C.byref(sh), C.byref(cf), _rope(rope), x.data_ptr(), _ptr(ctx), C.byref(w),
+                                         C.byref(c), _ptr(y_ctx), C.byref(tr) if tr is not None else None,
+                                         ws.data_ptr(), ws.numel(), _stream(x)))
     cache.valid, cache.step = c.valid, c.step
     return cache.y, y_ctx, out
 
@@ -385,7 +417,7 @@ def static_scratch_bytes() -> int:
 
 
 def attn_full(x: torch.Tensor, weights: Dict[str, torch.Tensor], shape: Shape, cfg: Cfg,
-              ctx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+              ctx: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, rope: Optional[Rope] = None):
     """The uncached layer on the same input: (y [F, N, C], y_ctx)."""
     _need(x, shape.torch_dtype, "x")
     w = _weights(weights, shape)
@@ -398,8 +430,8 @@ def attn_full(x: torch.Tensor, weights: Dict[str, torch.Tensor], shape: Shape, c
         _need(ctx, shape.torch_dtype, "ctx")
         y_ctx = torch.empty((shape.n_ctx, shape.C), dtype=x.dtype, device=dev)
     sh, cf = shape.c(), cfg.c()
-    L.check(L.lib().oc_attn_full(C.byref(sh), C.byref(cf), x.data_ptr(), _ptr(ctx), C.byref(w), y.data_ptr(),
-                                 _ptr(y_ctx), ws.data_ptr(), ws.numel(), _stream(x)))
+    L.check(L.lib().oc_attn_full_rope(C.byref(sh), C.byref(cf), _rope(rope), x.data_ptr(), _ptr(ctx), C.byref(w),
+                                      y.data_ptr(), _ptr(y_ctx), ws.data_ptr(), ws.numel(), _stream(x)))
     return y, y_ctx
 
 

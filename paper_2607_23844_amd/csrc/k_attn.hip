@@ -308,6 +308,23 @@ bool attn_head_dim_supported(int dh) {
     }
 }
 
+// Rotates the main rows of the projected Q and K in place.
+static hipError_t rotate_qk(const Plan &p, const AttnArgs &a, hipStream_t st) {
+    if (a.rope == nullptr) return hipSuccess;
+    RopeArgs r;
+    r.q = r.qo = a.q;
+    r.k = r.ko = a.k;
+    r.ld_q = r.ld_k = r.ld_qo = r.ld_ko = p.hd;
+    r.heads = r.k_heads = p.heads;
+    r.rows = a.n_main;
+    r.idx = a.rope_idx != nullptr ? a.rope_idx : a.row_idx;
+    r.pos = nullptr;
+    r.tF = a.tF;
+    r.tN = a.tN;
+    r.inverse = 0;
+    return launch_rope(*a.rope, r, p.bf16 ? ROPE_F16 : ROPE_F32, st);
+}
+
 hipError_t launch_attention(const Plan &p, const AttnArgs &a, hipStream_t st) {
     const int n_rows = a.seq_off != nullptr ? a.n_main : a.n_seq * a.L + a.n_ctx;
     const int Lk = a.L + (a.n_seq == 1 ? a.n_ctx : 0);
@@ -320,7 +337,7 @@ hipError_t launch_attention(const Plan &p, const AttnArgs &a, hipStream_t st) {
             return launch_proj_out(p, n_rows, a, st);
         }
         e = launch_proj_qkv(p, rm, a, st);   // (converts wo when no earlier launch has)
-        if (e != hipSuccess) return e;
+        if (e != hipSuccess || (e = rotate_qk(p, a, st)) != hipSuccess) return e;
         if ((e = launch_flash(p, a, Lk, st)) != hipSuccess) return e;
         AttnArgs o = a;
         o.wo16_ready = 1;
@@ -334,6 +351,7 @@ hipError_t launch_attention(const Plan &p, const AttnArgs &a, hipStream_t st) {
                                          : go_proj_f32<F32Small, 32>(p, a, rm, st);
         if (e != hipSuccess) return e;
     }
+    if ((e = rotate_qk(p, a, st)) != hipSuccess) return e;
     {
         StageScope _stage(st, "attn_f32");
         if ((e = launch_attn_f32(p, a, Lk, st)) != hipSuccess) return e;

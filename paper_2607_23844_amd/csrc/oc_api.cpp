@@ -554,8 +554,20 @@ oc_status oc_gather(const oc_shape *shape, const oc_cfg *cfg, const void *x, con
 oc_status oc_attn_reduced(const oc_shape *shape, const void *x_kept, int32_t n_seq, int32_t seq_len, const void *ctx,
                           const oc_attn_weights *w, void *y_kept, void *y_ctx, void *ws, size_t ws_bytes,
                           hipStream_t stream) {
+    return oc_attn_reduced_rope(shape, nullptr, nullptr, x_kept, n_seq, seq_len, ctx, w, y_kept, y_ctx, ws, ws_bytes,
+                                stream);
+}
+
+oc_status oc_attn_reduced_rope(const oc_shape *shape, const oc_rope *rope, const int32_t *kept_idx,
+                               const void *x_kept, int32_t n_seq, int32_t seq_len, const void *ctx,
+                               const oc_attn_weights *w, void *y_kept, void *y_ctx, void *ws, size_t ws_bytes,
+                               hipStream_t stream) {
     oc_status s = check_shape(shape);
     if (s != OC_OK) return s;
+    RopeGeom rg;
+    if ((s = make_rope(shape, rope, rg)) != OC_OK) return s;
+    if (rope && (long long)n_seq * seq_len > 0 && !kept_idx)
+        return fail(OC_ERR_INVALID_ARG, "rotary positions need the rows' tokens: kept_idx is NULL");
     if (n_seq < 0 || seq_len < 0) return fail(OC_ERR_SHAPE, "n_seq and seq_len must be >= 0");
     if ((long long)n_seq * seq_len + shape->n_ctx >= (1LL << 30)) return fail(OC_ERR_SHAPE, "batch too large");
     if (shape->n_ctx > 0 && n_seq != 1) return fail(OC_ERR_SHAPE, "context tokens need exactly one sequence");
@@ -584,6 +596,8 @@ oc_status oc_attn_reduced(const oc_shape *shape, const void *x_kept, int32_t n_s
     a.q = at<char>(ws, aw.q); a.k = at<char>(ws, aw.k); a.o = at<char>(ws, aw.o); a.vt = at<char>(ws, aw.v);
     a.lpad = aw.lpad;
     a.wo16 = at<char>(ws, aw.wo16);
+    a.rope = rope ? &rg : nullptr;
+    a.rope_idx = kept_idx;
     HIP_TRY(launch_attention(p, a, stream), "attention");
     return ok();
 }
@@ -606,8 +620,16 @@ oc_status oc_restore(const oc_shape *shape, const void *y_kept, int32_t n_rows, 
 oc_status oc_layer_cached(const oc_shape *shape, const oc_cfg *cfg, const void *x, const void *ctx,
                           const oc_attn_weights *w, oc_cache *cache, void *y_ctx, oc_trace *trace, void *ws,
                           size_t ws_bytes, hipStream_t stream) {
+    return oc_layer_cached_rope(shape, cfg, nullptr, x, ctx, w, cache, y_ctx, trace, ws, ws_bytes, stream);
+}
+
+oc_status oc_layer_cached_rope(const oc_shape *shape, const oc_cfg *cfg, const oc_rope *rope, const void *x,
+                               const void *ctx, const oc_attn_weights *w, oc_cache *cache, void *y_ctx,
+                               oc_trace *trace, void *ws, size_t ws_bytes, hipStream_t stream) {
     oc_status s = check_shape(shape);
     if (s != OC_OK) return s;
+    RopeGeom rg;
+    if ((s = make_rope(shape, rope, rg)) != OC_OK) return s;
     if ((s = check_cfg(cfg)) != OC_OK) return s;
     if (!cache || !cache->y) return fail(OC_ERR_CACHE_STATE, "cache or cache->y is NULL");
     if (cache->valid != 0 && cache->valid != 1) return fail(OC_ERR_CACHE_STATE, "cache->valid must be 0 or 1");
@@ -651,6 +673,7 @@ oc_status oc_layer_cached(const oc_shape *shape, const oc_cfg *cfg, const void *
     a.wo16 = at<char>(ws, aw.wo16);
     a.wo16_ready = wo_early ? 1 : 0;
     a.seq_off = p.kind == KIND_FPATCH ? at<int32_t>(ws, L.seqoff) : nullptr;
+    a.rope = rope ? &rg : nullptr;
     HIP_TRY(launch_attention(p, a, stream), "attention");
     if (map_matched) HIP_TRY(launch_copy_matched(p, cached, p.n_cached, rmap, kept, cache->y, stream), "copy matched");
 
@@ -782,9 +805,17 @@ size_t oc_static_scratch_bytes(void) { return OC_STATIC_SCRATCH_BYTES; }
 oc_status oc_attn_full(const oc_shape *shape, const oc_cfg *cfg, const void *x, const void *ctx,
                        const oc_attn_weights *w, void *y, void *y_ctx, void *ws, size_t ws_bytes,
                        hipStream_t stream) {
+    return oc_attn_full_rope(shape, cfg, nullptr, x, ctx, w, y, y_ctx, ws, ws_bytes, stream);
+}
+
+oc_status oc_attn_full_rope(const oc_shape *shape, const oc_cfg *cfg, const oc_rope *rope, const void *x,
+                            const void *ctx, const oc_attn_weights *w, void *y, void *y_ctx, void *ws,
+                            size_t ws_bytes, hipStream_t stream) {
     Plan p0;
     oc_status s = make_plan(shape, cfg, true, p0);
     if (s != OC_OK) return s;
+    RopeGeom rg;
+    if ((s = make_rope(shape, rope, rg)) != OC_OK) return s;
     if (!x || !y) return fail(OC_ERR_INVALID_ARG, "NULL pointer");
     if ((s = check_weights(w)) != OC_OK) return s;
     if (shape->n_ctx > 0 && (!ctx || !y_ctx)) return fail(OC_ERR_INVALID_ARG, "NULL ctx / y_ctx");
@@ -810,6 +841,7 @@ oc_status oc_attn_full(const oc_shape *shape, const oc_cfg *cfg, const void *x, 
     a.q = at<char>(ws, aw.q); a.k = at<char>(ws, aw.k); a.o = at<char>(ws, aw.o); a.vt = at<char>(ws, aw.v);
     a.lpad = aw.lpad;
     a.wo16 = at<char>(ws, aw.wo16);
+    a.rope = rope ? &rg : nullptr;
     HIP_TRY(launch_attention(p, a, stream), "attention");
     return ok();
 }

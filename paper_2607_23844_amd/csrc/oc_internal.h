@@ -5,6 +5,7 @@
 #include <cstddef>
 #include <cstdint>
 #include <hip/hip_runtime_api.h>
+#include "oc_ops.h"
 
 namespace oc {
 
@@ -207,6 +208,8 @@ struct AttnArgs {
     const int32_t *seq_off;           // sequences of varying length: sequence s owns rows
                                       // [seq_off[s], seq_off[s+1]) (n_main rows in all, no context,
                                       // L the longest); nullptr: every sequence has L rows
+    const RopeGeom *rope;             // rotary positions of the main rows' q and k, or NULL
+    const int32_t *rope_idx;          // row -> token for them (NULL: as the rows are read)
 };
 hipError_t launch_attention(const Plan &p, const AttnArgs &a, hipStream_t st);
 

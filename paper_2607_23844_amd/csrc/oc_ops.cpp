@@ -90,7 +90,84 @@ int vectors(const NormArgs &a, size_t esz, Range (&v)[7]) {
 
 }  // namespace
 
+namespace oc {
+
+oc_status make_rope(const oc_shape *sh, const oc_rope *rope, RopeGeom &g) {
+    if (!rope) return OC_OK;
+    long long sum = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (rope->dim[i] < 0 || rope->dim[i] % 2)
+            return failf(OC_ERR_SHAPE, "rotary dim[%d]=%d must be even and >= 0", i, rope->dim[i]);
+        if (!std::isfinite(rope->scale[i])) return failf(OC_ERR_INVALID_ARG, "rotary scale[%d] must be finite", i);
+        sum += rope->dim[i];
+    }
+    if (sum < 2 || sum > sh->head_dim)
+        return failf(OC_ERR_SHAPE, "rotary dims of %lld channels in all: outside [2, head_dim=%d]", sum, sh->head_dim);
+    if (rope->layout < OC_ROPE_PAIRS || rope->layout > OC_ROPE_SPLIT)
+        return failf(OC_ERR_INVALID_ARG, "unknown rotary layout %d", rope->layout);
+    if (rope->shared != 0 && rope->shared != 1) return failf(OC_ERR_INVALID_ARG, "shared must be 0 or 1");
+    if (!(rope->theta > 0.0) || !std::isfinite(rope->theta))
+        return failf(OC_ERR_INVALID_ARG, "theta=%g must be finite and > 0", rope->theta);
+    rope_geom(rope->dim, rope->layout, rope->shared, rope->origin, rope->theta, rope->scale, sh->F, sh->H, sh->W,
+              sh->head_dim, g);
+    for (int p = 0; p < g.P; ++p)
+        if (!std::isfinite(g.turn[p] * 0x1p33))   // (any position plus origin)
+            return failf(OC_ERR_INVALID_ARG, "theta=%g and the scales give pair %d no finite angle", rope->theta, p);
+    return OC_OK;
+}
+
+}  // namespace oc
+
 extern "C" {
+
+oc_status oc_rope_qk(const oc_shape *shape, const oc_rope *rope, int32_t n_rows, const int32_t *kept_idx,
+                     const int32_t *pos, const void *q, int64_t ld_q, const void *k, int64_t ld_k, int32_t k_heads,
+                     void *q_out, int64_t ld_qo, void *k_out, int64_t ld_ko, int32_t inverse, hipStream_t stream) {
+    oc_status s = valid_shape(shape);
+    if (s != OC_OK) return s;
+    if (!rope) return failf(OC_ERR_INVALID_ARG, "rope is NULL");
+    RopeGeom g;
+    if ((s = make_rope(shape, rope, g)) != OC_OK) return s;
+    if (n_rows < 0 || n_rows >= (1 << 30)) return failf(OC_ERR_SHAPE, "n_rows=%d outside [0, 2^30)", n_rows);
+    if (inverse != 0 && inverse != 1) return failf(OC_ERR_INVALID_ARG, "inverse must be 0 or 1");
+    if (kept_idx && pos) return failf(OC_ERR_INVALID_ARG, "kept_idx and pos exclude each other");
+    if (!kept_idx && !pos && n_rows > g.FN)
+        return failf(OC_ERR_SHAPE, "n_rows=%d past the grid of %ld tokens", n_rows, g.FN);
+    if (n_rows > 0 && !q && !k) return failf(OC_ERR_INVALID_ARG, "neither q nor k is given");
+    if ((q && !q_out) || (!q && q_out) || (k && !k_out) || (!k && k_out))
+        return failf(OC_ERR_INVALID_ARG, "q and q_out, k and k_out go together");
+    if (k && (k_heads < 1 || k_heads > (1 << 20))) return failf(OC_ERR_SHAPE, "k_heads=%d outside [1, 2^20]", k_heads);
+    const bool bf16 = shape->dtype == OC_BF16;
+    const size_t esz = bf16 ? 2 : 4;
+    struct Side { const void *p; int64_t ld; size_t width; const char *name; };
+    const size_t wq = (size_t)shape->heads * shape->head_dim, wk = k ? (size_t)k_heads * shape->head_dim : 0;
+    const Side in[2] = {{q, ld_q, wq, "q"}, {k, ld_k, wk, "k"}}, out[2] = {{q_out, ld_qo, wq, "q_out"},
+                                                                         {k_out, ld_ko, wk, "k_out"}};
+    for (const Side &d : {in[0], in[1], out[0], out[1]}) {
+        if (!d.p) continue;
+        if (!is_aligned(d.p, 16)) return failf(OC_ERR_INVALID_ARG, "%s must be 16-byte aligned", d.name);
+        if (d.ld < (int64_t)d.width || d.ld > (1LL << 40) || d.ld * esz % 16)
+            return failf(OC_ERR_SHAPE, "%s: a row stride of %lld elements is not a multiple of 16 bytes of at least %zu",
+                         d.name, (long long)d.ld, d.width);
+    }
+    for (const Side &o : out) {
+        for (const Side &i : in)
+            if (!(i.p == o.p && i.ld == o.ld && i.width == o.width) &&
+                rows_overlap(i.p, i.width * esz, i.ld * esz, o.p, o.width * esz, o.ld * esz, n_rows))
+                return failf(OC_ERR_INVALID_ARG, "%s overlaps %s", o.name, i.name);
+        if (overlaps(kept_idx, (size_t)n_rows * 4, o.p, n_rows ? ((n_rows - 1) * o.ld + o.width) * esz : 0) ||
+            overlaps(pos, (size_t)n_rows * 12, o.p, n_rows ? ((n_rows - 1) * o.ld + o.width) * esz : 0))
+            return failf(OC_ERR_INVALID_ARG, "%s overlaps the positions", o.name);
+    }
+    if (rows_overlap(q_out, wq * esz, ld_qo * esz, k_out, wk * esz, ld_ko * esz, n_rows))
+        return failf(OC_ERR_INVALID_ARG, "q_out overlaps k_out");
+    if (q && k && (q == k_out || k == q_out) && n_rows > 0)
+        return failf(OC_ERR_INVALID_ARG, "an output is the other tensor's input");
+    if (n_rows == 0) return record_error(OC_OK, "");
+    const RopeArgs a{q, k, q_out, k_out, (long)ld_q, (long)ld_k, (long)ld_qo, (long)ld_ko, shape->heads, k_heads,
+                     n_rows, kept_idx, pos, 0, 0, inverse};
+    return launched(launch_rope(g, a, bf16 ? ROPE_BF16 : ROPE_F32, stream), "rope");
+}
 
 oc_status oc_norm_gate(const oc_shape *shape, int32_t n_rows, const void *x, const void *y, const oc_norm *post,
                        const oc_norm *pre, const oc_mod *mod, float res_scale, void *h, void *n, hipStream_t stream) {

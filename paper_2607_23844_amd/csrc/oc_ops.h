@@ -1,5 +1,5 @@
 // Argument structures and launchers of the operators around a sublayer
-// (k_norm.hip).
+// (k_norm.hip, k_rope.hip).
 #pragma once
 #include <cstddef>
 #include <cstdint>
@@ -25,5 +25,37 @@ hipError_t launch_norm_gate_grad(const NormArgs &a, const void *dh, const void *
                                  const NormGrads &g, void *ws, hipStream_t st);
 hipError_t launch_zero(float *p, int n, hipStream_t st);   // gradients summed over no rows
 size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod);
+
+
+// Rotary positions, the geometry of one head as a kernel takes it: pairs 0..P
+// of the axes in order, then those past the rotated channels (left alone) up
+// to dh / 2.
+constexpr int ROPE_MAX_PAIRS = 64;
+struct RopeGeom {
+    int P, dh;               // rotated pairs, head dim
+    int axis1, axis2;        // first pair of the second and of the third axis
+    int pairs;               // neighbours (2p, 2p + 1); else halves:
+    int sect[5];             // pairs [sect[i], sect[i + 1]) lie in two halves from channel 2 sect[i] on
+    int vec;                 // largest power of two <= 8 that divides every sect
+    int N, W;
+    long FN;                 // tokens of the grid
+    double origin[3];
+    double turn[ROPE_MAX_PAIRS];   // turns (of 2 pi) per position
+};
+// fills g from checked arguments
+void rope_geom(const int *dim, int layout, int shared, const int *origin, double theta, const double *scale, int F,
+               int H, int W, int head_dim, RopeGeom &g);
+
+enum RopeType { ROPE_BF16, ROPE_F16, ROPE_F32 };
+struct RopeArgs {
+    const void *q, *k;       // either may be NULL
+    void *qo, *ko;
+    long ld_q, ld_k, ld_qo, ld_ko;
+    int heads, k_heads, rows;
+    const int *idx, *pos;    // row -> token, or row -> position, or NULL
+    int tF, tN;              // tF > 0 (no idx): row n*tF + f is token f*tN + n
+    int inverse;
+};
+hipError_t launch_rope(const RopeGeom &g, const RopeArgs &a, RopeType type, hipStream_t st);
 
 }  // namespace oc

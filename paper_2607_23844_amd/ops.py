@@ -1,5 +1,6 @@
 """The operators around a sublayer, with the names of the C ABI (include/oc.h):
-norms fused with gate, modulation and residual, and their gradients.
+norms fused with gate, modulation and residual, and their gradients; rotary
+positions.
 
 As in api.py this is argument marshalling only.  Tensors are on one GPU, which
 need not be the current one; the work goes on that GPU's current stream.
@@ -9,12 +10,12 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 from dataclasses import dataclass
-from typing import Dict, Optional, Sequence
+from typing import Dict, Optional, Sequence, Tuple
 
 import torch
 
 from . import _lib as L
-from .api import Shape, _ptr
+from .api import Rope, Shape, _ptr
 
 
 @dataclass
@@ -193,3 +194,56 @@ def norm_gate_grad(x: torch.Tensor, shape: Shape, dn: Optional[torch.Tensor] = N
                                           _ptr(out["dx"]), _ptr(out["dy"]), C.byref(g), ws.data_ptr(),
                                           ws.numel() * ws.element_size(), _stream_of(x)))
     return out
+
+
+def _heads_of(t: Optional[torch.Tensor], rows: Optional[int], heads: Optional[int], shape: Shape, dev, name: str):
+    """(address, row stride, heads) of a [rows, heads, head_dim] tensor whose
+    rows hold their heads contiguously."""
+    if t is None:
+        return None, 0, 0
+    if _gpu(t, name).dtype != shape.torch_dtype:
+        raise _bad(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected {shape.torch_dtype}")
+    if dev is not None and t.device != dev:
+        raise _bad(L.OC_ERR_INVALID_ARG, f"{name} is on {t.device}, expected {dev}")
+    if t.dim() != 3 or t.shape[2] != shape.head_dim or (rows is not None and t.shape[0] != rows) or \
+            (heads is not None and t.shape[1] != heads):
+        raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(t.shape)}, expected "
+                                   f"{('rows' if rows is None else rows, 'heads' if heads is None else heads, shape.head_dim)}")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != shape.head_dim):
+        raise _bad(L.OC_ERR_INVALID_ARG, f"the heads of a row of {name} must be contiguous")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2], t.shape[1]
+
+
+def _ids(t: Optional[torch.Tensor], shape, dev, name: str) -> Optional[int]:
+    return _like(t, torch.Size(shape), torch.int32, dev, name)
+
+
+def rope_qk(q: Optional[torch.Tensor], k: Optional[torch.Tensor], rope: Rope, shape: Shape,
+            kept_idx: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None, inverse: bool = False,
+            q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None
+            ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """oc_rope_qk: q [rows, heads, head_dim] and k [rows, k_heads, head_dim]
+    (rows may be columns of a wider buffer) turned by their tokens' positions:
+    token kept_idx[r] (None: r) of the shape's grid, or pos [rows, 3] int32.
+    inverse: turned back, which is also the gradient.  q_out and k_out: new
+    contiguous tensors unless given (q and k themselves: in place)."""
+    first = q if q is not None else k
+    if first is None:
+        raise _bad(L.OC_ERR_INVALID_ARG, "neither q nor k is given")
+    rows, dev = _gpu(first, "q").shape[0], first.device
+    qp, ldq, _ = _heads_of(q, rows, shape.heads, shape, dev, "q")
+    kp, ldk, kh = _heads_of(k, rows, None, shape, dev, "k")
+    if q_out is None and q is not None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if k_out is None and k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
+    qop, ldqo, _ = _heads_of(q_out, rows, shape.heads, shape, dev, "q_out")
+    kop, ldko, _ = _heads_of(k_out, rows, kh, shape, dev, "k_out")
+    ip, pp = _ids(kept_idx, (rows,), dev, "kept_idx"), _ids(pos, (rows, 3), dev, "pos")
+    if rows == 0:      # (empty tensors have no address)
+        qp = kp = qop = kop = None
+    sh, ro = shape.c(), rope.c()
+    with _on(first):
+        L.check(L.lib().oc_rope_qk(C.byref(sh), C.byref(ro), rows, ip, pp, qp, ldq, kp, ldk, kh, qop, ldqo, kop, ldko,
+                                   1 if inverse else 0, _stream_of(first)))
+    return q_out, k_out

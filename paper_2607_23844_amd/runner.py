@@ -9,15 +9,16 @@ from typing import Dict, Optional
 import torch
 
 from . import _lib as L
-from .api import Cfg, LayerCache, Shape, _need, _stream, _weights, workspace
+from .api import Cfg, LayerCache, Rope, Shape, _need, _stream, _weights, workspace
 
 
 class LayerRunner:
-    """oc_layer_cached on a fixed shape, cfg, weights, cache and workspace."""
+    """oc_layer_cached (with rope: oc_layer_cached_rope) on a fixed shape, cfg, weights, cache and workspace."""
 
     def __init__(self, shape: Shape, cfg: Cfg, weights: Dict[str, torch.Tensor], device,
-                 ctx: Optional[torch.Tensor] = None):
+                 ctx: Optional[torch.Tensor] = None, rope: Optional[Rope] = None):
         self.shape, self.cfg = shape, cfg
+        self._rope = rope.c() if rope is not None else None
         self._w = _weights(weights, shape)
         self.weights = weights
         self.cache = LayerCache(shape, device)
@@ -30,7 +31,8 @@ class LayerRunner:
         self._sh, self._cf = shape.c(), cfg.c()
         self._c = L.oc_cache(self.cache.y.data_ptr(), 0, 0)
         self._stream = _stream(self.cache.y)
-        self._fn = L.lib().oc_layer_cached
+        self._fn = L.lib().oc_layer_cached_rope
+        self._ro = C.byref(self._rope) if rope is not None else None
         self._args_tail = (C.byref(self._w), C.byref(self._c), self.y_ctx.data_ptr() if self.y_ctx is not None else None,
                            None, self.ws.data_ptr(), self.ws.numel(), self._stream)
         self._ctx_ptr = ctx.data_ptr() if ctx is not None else None
@@ -45,7 +47,7 @@ class LayerRunner:
         self._args_tail = self._args_tail[:-1] + (self._stream,)
 
     def __call__(self, x: torch.Tensor) -> torch.Tensor:
-        st = self._fn(C.byref(self._sh), C.byref(self._cf), x.data_ptr(), self._ctx_ptr, *self._args_tail)
+        st = self._fn(C.byref(self._sh), C.byref(self._cf), self._ro, x.data_ptr(), self._ctx_ptr, *self._args_tail)
         if st != 0:
             L.check(st)
         self.cache.valid, self.cache.step = self._c.valid, self._c.step
@@ -53,10 +55,12 @@ class LayerRunner:
 
 
 class FullRunner:
-    """oc_attn_full (the uncached layer) on a fixed shape, weights and workspace."""
+    """oc_attn_full or oc_attn_full_rope (the uncached layer) on a fixed shape, weights and workspace."""
 
     def __init__(self, shape: Shape, cfg: Cfg, weights: Dict[str, torch.Tensor], device,
-                 ctx: Optional[torch.Tensor] = None):
+                 ctx: Optional[torch.Tensor] = None, rope: Optional[Rope] = None):
+        self._rope = rope.c() if rope is not None else None
+        self._ro = C.byref(self._rope) if rope is not None else None
         self._w = _weights(weights, shape)
         self.weights = weights
         self.ws = workspace(shape, cfg, device)
@@ -65,7 +69,7 @@ class FullRunner:
         if shape.n_ctx > 0:
             self.y_ctx = torch.empty((shape.n_ctx, shape.C), dtype=shape.torch_dtype, device=device)
         self._sh, self._cf = shape.c(), cfg.c()
-        self._fn = L.lib().oc_attn_full
+        self._fn = L.lib().oc_attn_full_rope
         self._ctx_ptr = ctx.data_ptr() if ctx is not None else None
         self._tail = (C.byref(self._w), self.y.data_ptr(), self.y_ctx.data_ptr() if self.y_ctx is not None else None,
                       self.ws.data_ptr(), self.ws.numel(), _stream(self.y))
@@ -75,7 +79,7 @@ class FullRunner:
         self._tail = self._tail[:-1] + (_stream(self.y),)
 
     def __call__(self, x: torch.Tensor) -> torch.Tensor:
-        st = self._fn(C.byref(self._sh), C.byref(self._cf), x.data_ptr(), self._ctx_ptr, *self._tail)
+        st = self._fn(C.byref(self._sh), C.byref(self._cf), self._ro, x.data_ptr(), self._ctx_ptr, *self._tail)
         if st != 0:
             L.check(st)
         return self.y

@@ -107,6 +107,36 @@ class NormGate:
         return out
 
 
+def rope_pairs(dims, layout, shared):
+    """[(first channel, second channel, axis, exponent of 1 / theta)]"""
+    out, start, P = [], 0, sum(dims) // 2
+    for a, n in enumerate(dims):
+        for i in range(n // 2):
+            p = start // 2 + i
+            ab = {"pairs": (2 * p, 2 * p + 1), "halves": (start + i, start + n // 2 + i), "split": (p, p + P)}[layout]
+            out.append((*ab, a, p / P if shared else 2 * i / n))
+        start += n
+    return out
+
+
+def rope(v, pos, rp, inverse=False):
+    """v [rows, heads, head_dim] turned by positions [rows, 3] under an
+    oc.Rope: (value, size)."""
+    v, pos = d(v), d(pos)
+    o, z = v.clone(), v.abs()
+    for a, b, axis, e in rope_pairs(rp.dims, rp.layout, rp.shared):
+        ang = ((pos[:, axis] + rp.origin[axis]) * rp.scale[axis] * rp.theta ** -e)[:, None]
+        c, s = ang.cos(), -ang.sin() if inverse else ang.sin()
+        o[..., a], o[..., b] = v[..., a] * c - v[..., b] * s, v[..., a] * s + v[..., b] * c
+        z[..., a] = z[..., b] = v[..., a].abs() + v[..., b].abs()
+    return o, z
+
+
+def grid_pos(tokens, H, W):
+    t = d(tokens).long()
+    return torch.stack([t // (H * W), t % (H * W) // W, t % (H * W) % W], 1).double()
+
+
 def check(got, ref, size, roundings, what):
     """|got - ref| <= the output's own rounding + roundings 2^-24 size."""
     got = got.detach().cpu()

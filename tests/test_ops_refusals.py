@@ -148,3 +148,79 @@ def test_norm_formulas_against_differences(pre, post):
             val.append(float((o.h * dh + o.n * dn).sum()))
         along = 2 * float((got["d" + k if k in "xy" else k][0].reshape(by.shape) * by).sum())
         assert abs(val[0] - val[1] - along) <= 1e-6 * (abs(along) + 1e-5), k
+
+
+def rope_call(shape=None, rope=oc.Rope((0, 32, 32)), rows=4, idx=None, pos=None, q=at(0), ld_q=128, k=at(1), ld_k=128,
+              kh=2, qo=at(2), ld_qo=128, ko=at(3), ld_ko=128, inverse=0, **fields):
+    sh = (shape or oc.Shape(1, 4, 4, 128, 2, 64, 0, "bf16")).c()
+    ro = None if rope is None else rope.c()
+    for name, v in fields.items():
+        setattr(ro, name, v)
+    return L.lib().oc_rope_qk(C.byref(sh), None if ro is None else C.byref(ro), rows, idx, pos, q, ld_q, k, ld_k, kh,
+                              qo, ld_qo, ko, ld_ko, inverse, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(rope=None), L.OC_ERR_INVALID_ARG),
+    (dict(rope=oc.Rope((0, 31, 32))), L.OC_ERR_SHAPE),
+    (dict(rope=oc.Rope((-2, 32, 32))), L.OC_ERR_SHAPE),
+    (dict(rope=oc.Rope((2, 32, 32))), L.OC_ERR_SHAPE),                           # more than the head
+    (dict(rope=oc.Rope((1 << 30, 1 << 30, 1 << 30))), L.OC_ERR_SHAPE),
+    (dict(rope=oc.Rope((0, 0, 0))), L.OC_ERR_SHAPE),
+    (dict(rope=oc.Rope((0, 32, 32), theta=0.0)), L.OC_ERR_INVALID_ARG),
+    (dict(rope=oc.Rope((0, 32, 32), theta=-1.0)), L.OC_ERR_INVALID_ARG),
+    (dict(rope=oc.Rope((0, 32, 32), theta=float("inf"))), L.OC_ERR_INVALID_ARG),
+    (dict(rope=oc.Rope((0, 32, 32), scale=(1.0, float("nan"), 1.0))), L.OC_ERR_INVALID_ARG),
+    (dict(rope=oc.Rope((0, 32, 32), scale=(1.0, 1.0, 1e308))), L.OC_ERR_INVALID_ARG),
+    (dict(layout=3), L.OC_ERR_INVALID_ARG),
+    (dict(shared=2), L.OC_ERR_INVALID_ARG),
+    (dict(rows=-1), L.OC_ERR_SHAPE),
+    (dict(rows=17), L.OC_ERR_SHAPE),                                             # past the grid
+    (dict(rows=1 << 30, idx=at(5)), L.OC_ERR_SHAPE),
+    (dict(idx=at(5), pos=at(6)), L.OC_ERR_INVALID_ARG),
+    (dict(inverse=2), L.OC_ERR_INVALID_ARG),
+    (dict(q=None, qo=None, k=None, ko=None), L.OC_ERR_INVALID_ARG),
+    (dict(qo=None), L.OC_ERR_INVALID_ARG),
+    (dict(k=None), L.OC_ERR_INVALID_ARG),
+    (dict(kh=0), L.OC_ERR_SHAPE),
+    (dict(kh=3), L.OC_ERR_SHAPE),                                                # wider than its rows
+    (dict(ld_q=120), L.OC_ERR_SHAPE),
+    (dict(ld_qo=132), L.OC_ERR_SHAPE),
+    (dict(q=at(0) + 2), L.OC_ERR_INVALID_ARG),
+    (dict(ko=at(3) + 8), L.OC_ERR_INVALID_ARG),
+    (dict(qo=at(0) + 256), L.OC_ERR_INVALID_ARG),                                # the next row of q
+    (dict(qo=at(0), ld_qo=136), L.OC_ERR_INVALID_ARG),                           # in place with another stride
+    (dict(qo=at(1)), L.OC_ERR_INVALID_ARG),
+    (dict(ko=at(0)), L.OC_ERR_INVALID_ARG),
+    (dict(qo=at(1), ko=at(0)), L.OC_ERR_INVALID_ARG),
+    (dict(ko=at(2)), L.OC_ERR_INVALID_ARG),
+    (dict(q=at(0), ld_q=256, qo=at(0), ld_qo=256, k=at(0) + 128, ld_k=256, ko=at(0) + 128, ld_ko=256),
+     L.OC_ERR_INVALID_ARG),                                                      # columns that share channels
+    (dict(idx=at(2)), L.OC_ERR_INVALID_ARG),
+    (dict(shape=oc.Shape(1, 4, 4, 128, 2, 60, 0, "bf16")), L.OC_ERR_SHAPE),
+])
+def test_rope_refuses(kw, status):
+    assert rope_call(**kw) == status
+
+
+def test_rope_struct_and_layer_calls_refuse():
+    assert C.sizeof(L.oc_rope) == 64
+    lib = L.lib()
+    sh, cf = oc.Shape(1, 8, 8, 32, 2, 16, 0, "bf16").c(), oc.Cfg("token", r=0.5).c()
+    bad, good = oc.Rope((0, 16, 16)).c(), oc.Rope((0, 8, 8)).c()
+    w, cache = L.oc_attn_weights(at(0), at(1), at(2), at(3)), L.oc_cache(at(5), 0, 0)
+    assert lib.oc_layer_cached_rope(C.byref(sh), C.byref(cf), C.byref(bad), at(4), None, C.byref(w), C.byref(cache),
+                                    None, None, at(6), 1 << 40, None) == L.OC_ERR_SHAPE
+    assert (cache.valid, cache.step) == (0, 0)
+    assert lib.oc_attn_full_rope(C.byref(sh), C.byref(cf), C.byref(bad), at(4), None, C.byref(w), at(5), None, at(6),
+                                 1 << 40, None) == L.OC_ERR_SHAPE
+    assert lib.oc_attn_reduced_rope(C.byref(sh), C.byref(bad), at(7), at(4), 1, 4, None, C.byref(w), at(5), None,
+                                    at(6), 1 << 40, None) == L.OC_ERR_SHAPE
+    assert lib.oc_attn_reduced_rope(C.byref(sh), C.byref(good), None, at(4), 1, 4, None, C.byref(w), at(5), None,
+                                    at(6), 1 << 40, None) == L.OC_ERR_INVALID_ARG
+    with pytest.raises(oc.OmniCacheError):
+        oc.Rope((32, 32)).c()
+    with pytest.raises(oc.OmniCacheError):
+        oc.Rope((0, 32, 32), layout="spiral").c()
+    with pytest.raises(oc.OmniCacheError):
+        oc.rope_qk(None, None, oc.Rope((0, 32, 32)), oc.Shape(1, 4, 4, 128, 2, 64))
