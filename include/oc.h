@@ -532,6 +532,51 @@ oc_status oc_attn_full_rope(const oc_shape *shape, const oc_cfg *cfg, const oc_r
                             size_t ws_bytes, hipStream_t stream);
 
 /*
+ * Products in 8-bit integers: rows quantised with a scale each (tokens of
+ * activations, output channels of weights), multiplied exactly in 32-bit
+ * integers, scaled back.
+ */
+
+/* Bytes of a quantised row of K elements: K rounded up to a multiple of 16
+   (the elements past K are zero). */
+size_t oc_i8_row_bytes(int32_t K);
+
+/*
+ * oc_quant_rows — row r of n_rows is row s = row_idx[r] (r where row_idx is
+ * NULL) of x, n_src rows of K elements of type dtype, ld elements apart:
+ *   scale[r] = max|x_s| / 127,  q[r][k] = 127 x_s[k] / max|x_s| rounded to the
+ * nearest whole number, ties to even (the exact quotient; a row of zeros has
+ * scale 0 and zeros).  A row that holds a NaN or an infinity gets the scale
+ * NaN and zeros, so products of it are NaN.  q is [n_rows,
+ * oc_i8_row_bytes(K)].  Rows whose row_idx lies outside [0, n_src) are left as
+ * they were.  Weights [out, in] are quantised once by the same call.
+ * K a multiple of 8, 8 <= K <= 131056; ld >= K, ld elements a multiple of 16
+ * bytes; x and q 16-byte aligned, q and scale overlap nothing else.
+ */
+oc_status oc_quant_rows(int32_t dtype, const void *x, int64_t ld, int32_t n_src, int32_t K, const int32_t *row_idx,
+                        int32_t n_rows, int8_t *q, float *scale, hipStream_t stream);
+
+typedef enum { OC_ACT_NONE = 0, OC_ACT_GELU = 1 } oc_act;   /* GELU: the tanh form of oc_ffn_reduced */
+
+/*
+ * oc_linear_i8 — y[t_r][n] = act((sum_k q[r][k] w[n][k]) scale_q[r] scale_w[n]
+ * + bias[n]) for n_rows rows and N outputs, t_r = out_idx[r] (r where out_idx
+ * is NULL): with the attention's kept_idx as oc_quant_rows' row_idx and as
+ * out_idx, a sublayer of the retained tokens only, restored in place.  q and w
+ * are [n_rows] and [N] rows of oc_i8_row_bytes(K) bytes (zeros past K), the
+ * sums are exact 32-bit integers, the rest fp32, rounded once to y's type
+ * dtype (also that of bias, which may be NULL).  Rows of y are ld_y elements
+ * apart; rows t_r outside [0, n_out) are not written, nor any other row.  The
+ * same t_r twice: either row is kept.
+ * K as in oc_quant_rows, N a multiple of 8; q, w, scale_w, bias and y 16-byte
+ * aligned, ld_y >= N and a multiple of 16 bytes, y overlaps no input; without
+ * out_idx, n_rows <= n_out.
+ */
+oc_status oc_linear_i8(int32_t dtype, int32_t n_rows, int32_t K, int32_t N, const int8_t *q, const float *scale_q,
+                       const int8_t *w, const float *scale_w, const void *bias, int32_t act, const int32_t *out_idx,
+                       int32_t n_out, void *y, int64_t ld_y, hipStream_t stream);
+
+/*
  * Layered Cache schedule proposal (§3.4, Alg. 1), host only.  For each
  * candidate layer-timestep pair (l, t) the caller gives the latency L[l,t]
  * that reusing the cache there saves and the quality loss Q[l,t] it costs

@@ -40,8 +40,10 @@ from .api import (  # noqa: F401
 from .ops import (  # noqa: F401
     Mod,
     Norm,
+    linear_i8,
     norm_gate,
     norm_gate_grad,
     norm_gate_grad_workspace_bytes,
+    quant_rows,
     rope_qk,
 )

@@ -12,6 +12,7 @@ OC_OK, OC_ERR_INVALID_ARG, OC_ERR_SHAPE, OC_ERR_DTYPE, OC_ERR_WORKSPACE, OC_ERR_
 OC_F32, OC_BF16 = 0, 1
 GRANS = {"token": 0, "frame": 1, "block": 2, "frame_token": 3}
 COLDS = {"matched": 0, "full": 1}
+ACTS = {"none": 0, "gelu": 1}
 ROPE_LAYOUTS = {"pairs": 0, "halves": 1, "split": 2}
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 
@@ -126,6 +127,12 @@ _SIGS = {
                                        C.c_size_t, C.c_void_p]),
     "oc_attn_full_rope": (C.c_int, [P(oc_shape), P(oc_cfg), P(oc_rope), C.c_void_p, C.c_void_p, P(oc_attn_weights),
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "oc_i8_row_bytes": (C.c_size_t, [C.c_int32]),
+    "oc_quant_rows": (C.c_int, [C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_int32,
+                                C.c_void_p, C.c_void_p, C.c_void_p]),
+    "oc_linear_i8": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                               C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int64,
+                               C.c_void_p]),
     "oc_block_cached": (C.c_int, [P(oc_shape), P(oc_cfg), P(oc_cfg), C.c_void_p, P(oc_attn_weights),
                                   P(oc_attn_weights), P(oc_cache), P(oc_cache), C.c_void_p, P(oc_trace), P(oc_trace),
                                   C.c_void_p, C.c_size_t, C.c_void_p]),

@@ -88,6 +88,18 @@ int vectors(const NormArgs &a, size_t esz, Range (&v)[7]) {
     return 7;
 }
 
+constexpr int MAX_ROWS = 1 << 30;
+constexpr int64_t MAX_LD = 1LL << 40;
+constexpr int MAX_I8_K = 131056;   // 128 * 128 * K stays below 2^31
+
+oc_status check_i8(int32_t dtype, int32_t n_rows, int32_t K) {
+    if (dtype != OC_F32 && dtype != OC_BF16) return failf(OC_ERR_DTYPE, "unknown dtype %d", dtype);
+    if (n_rows < 0 || n_rows >= MAX_ROWS) return failf(OC_ERR_SHAPE, "n_rows=%d outside [0, 2^30)", n_rows);
+    if (K < 8 || K % 8 || K > MAX_I8_K)
+        return failf(OC_ERR_SHAPE, "K=%d must be a multiple of 8 in [8, %d]", K, MAX_I8_K);
+    return OC_OK;
+}
+
 }  // namespace
 
 namespace oc {
@@ -251,6 +263,63 @@ oc_status oc_norm_gate_grad(const oc_shape *shape, int32_t n_rows, const void *x
     }
     const NormGrads ng{g.gate, g.scale, g.shift, g.post_w, g.post_b, g.pre_w, g.pre_b};
     return launched(launch_norm_gate_grad(a, dh, dn, dx, dy, ng, ws, stream), "norm_gate_grad");
+}
+
+size_t oc_i8_row_bytes(int32_t K) { return K > 0 ? (size_t)i8_row(K) : 0; }
+
+oc_status oc_quant_rows(int32_t dtype, const void *x, int64_t ld, int32_t n_src, int32_t K, const int32_t *row_idx,
+                        int32_t n_rows, int8_t *q, float *scale, hipStream_t stream) {
+    oc_status s = check_i8(dtype, n_rows, K);
+    if (s != OC_OK) return s;
+    const size_t esz = dtype == OC_BF16 ? 2 : 4;
+    if (n_src < 0 || n_src >= MAX_ROWS) return failf(OC_ERR_SHAPE, "n_src=%d outside [0, 2^30)", n_src);
+    if (!row_idx && n_rows > n_src) return failf(OC_ERR_SHAPE, "n_rows=%d of a matrix of %d rows", n_rows, n_src);
+    if (ld < K || ld > MAX_LD || ld * esz % 16)
+        return failf(OC_ERR_SHAPE, "x: a row stride of %lld elements is not a multiple of 16 bytes of at least K=%d",
+                     (long long)ld, K);
+    if (n_rows > 0 && (!q || !scale || (!x && n_src > 0))) return failf(OC_ERR_INVALID_ARG, "NULL pointer");
+    if (!is_aligned(x, 16) || !is_aligned(q, 16)) return failf(OC_ERR_INVALID_ARG, "x and q must be 16-byte aligned");
+    if (!is_aligned(scale, 4) || !is_aligned(row_idx, 4))
+        return failf(OC_ERR_INVALID_ARG, "scale and row_idx must be 4-byte aligned");
+    const size_t xb = n_src > 0 ? ((size_t)(n_src - 1) * ld + K) * esz : 0, qb = (size_t)n_rows * i8_row(K);
+    const size_t sb = (size_t)n_rows * 4;
+    if (overlaps(q, qb, x, xb) || overlaps(scale, sb, x, xb) || overlaps(q, qb, scale, sb) ||
+        overlaps(q, qb, row_idx, sb) || overlaps(scale, sb, row_idx, sb))
+        return failf(OC_ERR_INVALID_ARG, "q and scale must not overlap each other or an input");
+    if (n_rows == 0 || n_src == 0) return record_error(OC_OK, "");
+    return launched(launch_quant(dtype == OC_BF16, x, (long)ld, n_src, K, row_idx, n_rows, q, scale, stream),
+                    "quant_rows");
+}
+
+oc_status oc_linear_i8(int32_t dtype, int32_t n_rows, int32_t K, int32_t N, const int8_t *q, const float *scale_q,
+                       const int8_t *w, const float *scale_w, const void *bias, int32_t act, const int32_t *out_idx,
+                       int32_t n_out, void *y, int64_t ld_y, hipStream_t stream) {
+    oc_status s = check_i8(dtype, n_rows, K);
+    if (s != OC_OK) return s;
+    const size_t esz = dtype == OC_BF16 ? 2 : 4;
+    if (N < 8 || N % 8 || N > (1 << 24)) return failf(OC_ERR_SHAPE, "N=%d must be a multiple of 8 in [8, 2^24]", N);
+    if (act != OC_ACT_NONE && act != OC_ACT_GELU) return failf(OC_ERR_INVALID_ARG, "unknown activation %d", act);
+    if (n_out < 0 || n_out >= MAX_ROWS) return failf(OC_ERR_SHAPE, "n_out=%d outside [0, 2^30)", n_out);
+    if (!out_idx && n_rows > n_out) return failf(OC_ERR_SHAPE, "n_rows=%d into %d rows", n_rows, n_out);
+    if (ld_y < N || ld_y > MAX_LD || ld_y * esz % 16)
+        return failf(OC_ERR_SHAPE, "y: a row stride of %lld elements is not a multiple of 16 bytes of at least N=%d",
+                     (long long)ld_y, N);
+    if (n_rows > 0 && (!q || !scale_q || !w || !scale_w || (!y && n_out > 0)))
+        return failf(OC_ERR_INVALID_ARG, "NULL pointer");
+    if (!is_aligned(q, 16) || !is_aligned(w, 16) || !is_aligned(scale_w, 16) || !is_aligned(bias, 16) ||
+        !is_aligned(y, 16))
+        return failf(OC_ERR_INVALID_ARG, "q, w, scale_w, bias and y must be 16-byte aligned");
+    if (!is_aligned(scale_q, 4) || !is_aligned(out_idx, 4))
+        return failf(OC_ERR_INVALID_ARG, "scale_q and out_idx must be 4-byte aligned");
+    const size_t row = (size_t)i8_row(K), yb = n_out > 0 ? ((size_t)(n_out - 1) * ld_y + N) * esz : 0;
+    const Range ins[] = {{q, n_rows * row}, {w, N * row}, {scale_q, (size_t)n_rows * 4}, {scale_w, (size_t)N * 4},
+                         {bias, N * esz}, {out_idx, (size_t)n_rows * 4}};
+    for (const Range &r : ins)
+        if (overlaps(y, yb, r.p, r.bytes)) return failf(OC_ERR_INVALID_ARG, "y must not overlap an input");
+    if (n_rows == 0 || n_out == 0) return record_error(OC_OK, "");
+    const LinearI8Args a{q, w, scale_q, scale_w, bias, out_idx, y, (long)ld_y, n_rows, K, N, n_out,
+                         act == OC_ACT_GELU ? 1 : 0, dtype == OC_BF16};
+    return launched(launch_linear_i8(a, stream), "linear_i8");
 }
 
 }  // extern "C"

@@ -1,5 +1,5 @@
 // Argument structures and launchers of the operators around a sublayer
-// (k_norm.hip, k_rope.hip).
+// (k_norm.hip, k_rope.hip, k_i8.hip).
 #pragma once
 #include <cstddef>
 #include <cstdint>
@@ -57,5 +57,22 @@ struct RopeArgs {
     int inverse;
 };
 hipError_t launch_rope(const RopeGeom &g, const RopeArgs &a, RopeType type, hipStream_t st);
+
+// Products in 8-bit integers.
+constexpr long i8_row(long K) { return (K + 15) / 16 * 16; }
+hipError_t launch_quant(bool bf16, const void *x, long ld, int n_src, int K, const int *idx, int rows, int8_t *q,
+                        float *scale, hipStream_t st);
+struct LinearI8Args {
+    const int8_t *q, *w;         // rows of i8_row(K) bytes
+    const float *sq, *sw;
+    const void *bias;            // [N] or NULL
+    const int *out_idx;          // row -> y row, or NULL
+    void *y;
+    long ld_y;
+    int rows, K, N, n_out;
+    int gelu;
+    bool bf16;
+};
+hipError_t launch_linear_i8(const LinearI8Args &a, hipStream_t st);
 
 }  // namespace oc

@@ -1,6 +1,6 @@
 """The operators around a sublayer, with the names of the C ABI (include/oc.h):
 norms fused with gate, modulation and residual, and their gradients; rotary
-positions.
+positions; products in 8-bit integers.
 
 As in api.py this is argument marshalling only.  Tensors are on one GPU, which
 need not be the current one; the work goes on that GPU's current stream.
@@ -247,3 +247,69 @@ def rope_qk(q: Optional[torch.Tensor], k: Optional[torch.Tensor], rope: Rope, sh
         L.check(L.lib().oc_rope_qk(C.byref(sh), C.byref(ro), rows, ip, pp, qp, ldq, kp, ldk, kh, qop, ldqo, kop, ldko,
                                    1 if inverse else 0, _stream_of(first)))
     return q_out, k_out
+
+
+_DTYPES = {torch.float32: L.OC_F32, torch.bfloat16: L.OC_BF16}
+
+
+def _matrix(t, name: str):
+    """(address, row stride) of a 2-D tensor with contiguous rows."""
+    if _gpu(t, name).dtype not in _DTYPES:
+        raise _bad(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected bfloat16 or float32")
+    if t.dim() != 2:
+        raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(t.shape)}, expected two dimensions")
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise _bad(L.OC_ERR_INVALID_ARG, f"the rows of {name} must be contiguous")
+    return t.data_ptr() or None, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def quant_rows(x: torch.Tensor, row_idx: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+               scale: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """oc_quant_rows: the rows row_idx (None: all) of x [n, K] in 8 bits.
+    Returns (q int8 [rows, K rounded up to 16], scale fp32 [rows]); x is about
+    q * scale.  Weights [out, in] are quantised by the same call, once."""
+    at, ld = _matrix(x, "x")
+    dev, (n, K) = x.device, x.shape
+    rows = n if row_idx is None else row_idx.numel()
+    ip = _ids(row_idx, (rows,), dev, "row_idx")
+    Kp = (K + 15) // 16 * 16
+    q = torch.empty((rows, Kp), dtype=torch.int8, device=dev) if q is None else q
+    scale = torch.empty((rows,), dtype=torch.float32, device=dev) if scale is None else scale
+    qp, sp = _like(q, (rows, Kp), torch.int8, dev, "q"), _like(scale, (rows,), torch.float32, dev, "scale")
+    with _on(x):
+        L.check(L.lib().oc_quant_rows(_DTYPES[x.dtype], at, ld, n, K, ip, rows, qp, sp, _stream_of(x)))
+    return q, scale
+
+
+def linear_i8(q: torch.Tensor, scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+              bias: Optional[torch.Tensor] = None, act: str = "none", out_idx: Optional[torch.Tensor] = None,
+              y: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """oc_linear_i8: act((q w^T) scale w_scale + bias) of quantised rows q
+    [rows, K'] and weights w [N, K'] (both as quant_rows gives them).  y: a
+    tensor to write, its rows out_idx (None: the first ones), whose other rows
+    stay as they are; or None: a new [rows, N] tensor of type dtype (bfloat16
+    unless given)."""
+    dev = _gpu(q, "q").device
+    if q.dim() != 2 or _gpu(w, "w").dim() != 2:
+        raise _bad(L.OC_ERR_SHAPE, "q and w must have two dimensions")
+    (rows, Kp), N = q.shape, w.shape[0]
+    if act not in L.ACTS:
+        raise _bad(L.OC_ERR_INVALID_ARG, f"unknown activation {act!r}")
+    if Kp % 16:
+        raise _bad(L.OC_ERR_SHAPE, f"q has {Kp} columns, expected a multiple of 16")
+    qp, wp = _like(q, (rows, Kp), torch.int8, dev, "q"), _like(w, (N, Kp), torch.int8, dev, "w")
+    sp = _like(scale, (rows,), torch.float32, dev, "scale")
+    swp = _like(w_scale, (N,), torch.float32, dev, "w_scale")
+    if y is None:
+        if out_idx is not None:
+            raise _bad(L.OC_ERR_INVALID_ARG, "out_idx needs y, the tensor whose rows it names")
+        y = torch.empty((rows, N), dtype=torch.bfloat16 if dtype is None else dtype, device=dev)
+    at, ld = _matrix(y, "y")
+    if y.device != dev or y.shape[1] != N or (dtype is not None and y.dtype != dtype):
+        raise _bad(L.OC_ERR_SHAPE, f"y is {tuple(y.shape)} {y.dtype} on {y.device}, expected [..., {N}] on {dev}")
+    bp = _like(bias, (N,), y.dtype, dev, "bias")
+    ip = _ids(out_idx, (rows,), dev, "out_idx")
+    with _on(q):
+        L.check(L.lib().oc_linear_i8(_DTYPES[y.dtype], rows, Kp, N, qp, sp, wp, swp, bp, L.ACTS[act], ip, y.shape[0],
+                                     at, ld, _stream_of(q)))
+    return y

@@ -145,3 +145,33 @@ def check(got, ref, size, roundings, what):
     bad = ~(err <= tol)
     assert not bad.any(), (what, int(bad.sum()), float((err / tol).nan_to_num(1e30).max()),
                            got[bad][:4].tolist(), ref[bad][:4].tolist())
+
+
+def quant(x):
+    """(whole numbers, scales) of rows in 64 bits: the quotient 127 x / max|x|
+    as a fraction of whole numbers would round it (doubles keep it apart from
+    every tie that it is not: the values have at most 24 bits)."""
+    x = d(x)
+    top = x.abs().amax(1, keepdim=True)
+    q = torch.where(top > 0, x * 127.0 / torch.where(top > 0, top, torch.ones_like(top)), torch.zeros_like(x))
+    return q.round(), (top[:, 0].float() / 127.0)
+
+
+def gelu(v):
+    return 0.5 * v * (1.0 + torch.tanh((2.0 / torch.pi) ** 0.5 * (v + 0.044715 * v ** 3)))
+
+
+def linear_i8(q, s, w, ws, bias=None, act="none"):
+    """(value, size) of the product of quantised rows."""
+    acc = d(q).float().double() @ d(w).t()
+    v = acc * d(s)[:, None] * d(ws)
+    size = v.abs()
+    if bias is not None:
+        v, size = v + d(bias), size + d(bias).abs()
+    if act == "gelu":
+        # |gelu'| <= 1.13; beside that the factor's own evaluation, whose exponent
+        # 2 sqrt(2/pi) (v + 0.044715 v^3) is off by a few roundings of itself (it counts where the
+        # factor is neither 0 nor 1: |v| below 8, an exponent below 50)
+        size = 1.13 * size + v.abs() * 50.0
+        v = gelu(v)
+    return v, size

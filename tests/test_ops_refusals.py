@@ -224,3 +224,79 @@ def test_rope_struct_and_layer_calls_refuse():
         oc.Rope((0, 32, 32), layout="spiral").c()
     with pytest.raises(oc.OmniCacheError):
         oc.rope_qk(None, None, oc.Rope((0, 32, 32)), oc.Shape(1, 4, 4, 128, 2, 64))
+
+
+def quant_call(dtype=1, x=at(0), ld=64, n_src=8, K=64, idx=None, rows=8, q=at(1), scale=at(2)):
+    return L.lib().oc_quant_rows(dtype, x, ld, n_src, K, idx, rows, q, scale, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=2), L.OC_ERR_DTYPE),
+    (dict(K=60, ld=64), L.OC_ERR_SHAPE),
+    (dict(K=0), L.OC_ERR_SHAPE),
+    (dict(K=131072, ld=131072), L.OC_ERR_SHAPE),
+    (dict(ld=56), L.OC_ERR_SHAPE),
+    (dict(ld=68), L.OC_ERR_SHAPE),
+    (dict(rows=-1), L.OC_ERR_SHAPE),
+    (dict(rows=9), L.OC_ERR_SHAPE),                       # more than there are
+    (dict(rows=1 << 30, idx=at(4)), L.OC_ERR_SHAPE),
+    (dict(n_src=-1, idx=at(4)), L.OC_ERR_SHAPE),
+    (dict(x=None), L.OC_ERR_INVALID_ARG),
+    (dict(q=None), L.OC_ERR_INVALID_ARG),
+    (dict(scale=None), L.OC_ERR_INVALID_ARG),
+    (dict(x=at(0) + 8), L.OC_ERR_INVALID_ARG),
+    (dict(q=at(1) + 8), L.OC_ERR_INVALID_ARG),
+    (dict(scale=at(2) + 2), L.OC_ERR_INVALID_ARG),
+    (dict(idx=at(4) + 1), L.OC_ERR_INVALID_ARG),
+    (dict(q=at(0)), L.OC_ERR_INVALID_ARG),                # in place
+    (dict(scale=at(1) + 64), L.OC_ERR_INVALID_ARG),
+    (dict(idx=at(2)), L.OC_ERR_INVALID_ARG),
+])
+def test_quant_rows_refuses(kw, status):
+    assert quant_call(**kw) == status
+
+
+def linear_call(dtype=1, rows=4, K=64, N=16, q=at(0), sq=at(1), w=at(2), sw=at(3), bias=None, act=0, idx=None,
+                n_out=4, y=at(4), ld_y=16):
+    return L.lib().oc_linear_i8(dtype, rows, K, N, q, sq, w, sw, bias, act, idx, n_out, y, ld_y, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=-1), L.OC_ERR_DTYPE),
+    (dict(rows=-1), L.OC_ERR_SHAPE),
+    (dict(rows=5), L.OC_ERR_SHAPE),
+    (dict(n_out=-1, idx=at(5)), L.OC_ERR_SHAPE),
+    (dict(K=4), L.OC_ERR_SHAPE),
+    (dict(K=131064), L.OC_ERR_SHAPE),                     # its rows hold 131072 elements
+    (dict(N=12), L.OC_ERR_SHAPE),
+    (dict(N=0), L.OC_ERR_SHAPE),
+    (dict(ld_y=8), L.OC_ERR_SHAPE),
+    (dict(ld_y=20), L.OC_ERR_SHAPE),
+    (dict(act=2), L.OC_ERR_INVALID_ARG),
+    (dict(q=None), L.OC_ERR_INVALID_ARG),
+    (dict(sq=None), L.OC_ERR_INVALID_ARG),
+    (dict(w=None), L.OC_ERR_INVALID_ARG),
+    (dict(sw=None), L.OC_ERR_INVALID_ARG),
+    (dict(y=None), L.OC_ERR_INVALID_ARG),
+    (dict(q=at(0) + 8), L.OC_ERR_INVALID_ARG),
+    (dict(sw=at(3) + 4), L.OC_ERR_INVALID_ARG),
+    (dict(sq=at(1) + 2), L.OC_ERR_INVALID_ARG),
+    (dict(bias=at(6) + 2), L.OC_ERR_INVALID_ARG),
+    (dict(y=at(4) + 2), L.OC_ERR_INVALID_ARG),
+    (dict(y=at(0)), L.OC_ERR_INVALID_ARG),
+    (dict(y=at(3)), L.OC_ERR_INVALID_ARG),
+    (dict(bias=at(4)), L.OC_ERR_INVALID_ARG),
+    (dict(idx=at(4)), L.OC_ERR_INVALID_ARG),
+])
+def test_linear_i8_refuses(kw, status):
+    assert linear_call(**kw) == status
+
+
+def test_i8_rows_and_empty_calls():
+    f = L.lib().oc_i8_row_bytes
+    assert [f(k) for k in (-8, 0, 8, 16, 24, 1536)] == [0, 0, 16, 16, 32, 1536]
+    assert quant_call(rows=0, q=None, scale=None) == L.OC_OK and linear_call(rows=0, y=None) == L.OC_OK
+    with pytest.raises(oc.OmniCacheError):
+        oc.quant_rows(torch.zeros(2, 64))
+    with pytest.raises(oc.OmniCacheError):
+        oc.linear_i8(*(torch.zeros(2, 64, dtype=torch.int8), torch.zeros(2)) * 2)
