@@ -568,7 +568,7 @@ typedef enum { OC_ACT_NONE = 0, OC_ACT_GELU = 1 } oc_act;   /* GELU: the tanh fo
  * dtype (also that of bias, which may be NULL).  Rows of y are ld_y elements
  * apart; rows t_r outside [0, n_out) are not written, nor any other row.  The
  * same t_r twice: either row is kept.
- * K as in oc_quant_rows, N a multiple of 8; q, w, scale_w, bias and y 16-byte
+ * K as in oc_quant_rows, N a multiple of 8, n_rows * N < 2^37; q, w, scale_w, bias and y 16-byte
  * aligned, ld_y >= N and a multiple of 16 bytes, y overlaps no input; without
  * out_idx, n_rows <= n_out.
  */

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_ffn_up(const uint16_t *__r
                                                 int n_rows, int FN, int C, const uint16_t *__restrict__ w1,
                                                 int hidden, int n_at, int n_bt, uint16_t *__restrict__ H,
                                                 const uint4 *__restrict__ w2, long n8, uint4 *__restrict__ w2h) {
-    using T = typename RingShape<ID, false>::Tile;
+    using T = typename RingShape<ID, RING_BF16>::Tile;
     constexpr int BA = T::BA, BB = T::BB;
     extern __shared__ __align__(16) uint16_t lds[];
     const int n_tiles = n_at * n_bt;
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_ffn_down(const uint16_t *_
                                                   const uint16_t *__restrict__ w2, int C,
                                                   const int32_t *__restrict__ idx, int scatter, int FN, int n_at,
                                                   int n_bt, uint16_t *__restrict__ y) {
-    using T = typename RingShape<ID, true>::Tile;
+    using T = typename RingShape<ID, RING_F16>::Tile;
     constexpr int BA = T::BA, BB = T::BB;
     extern __shared__ __align__(16) uint16_t lds[];
     int at, bt;
@@ -144,7 +144,7 @@ hipError_t launch_ffn(const FfnArgs &a, hipStream_t st) {
         const int id = ring_pick(a.C, [&](int BA, int BB) { return (long)cdiv(a.hidden, BA) * cdiv(a.n_rows, BB); });
         const hipError_t e = ring_dispatch(id, [&](auto c) -> hipError_t {
             constexpr int ID = decltype(c)::value;
-            using T = typename RingShape<ID, false>::Tile;
+            using T = typename RingShape<ID, RING_BF16>::Tile;
             const hipError_t el = allow_lds(k_ffn_up<ID>, T::LDS_BYTES);
             if (el != hipSuccess) return el;
             const int n_at = cdiv(a.hidden, T::BA), n_bt = cdiv(a.n_rows, T::BB);
@@ -160,7 +160,7 @@ hipError_t launch_ffn(const FfnArgs &a, hipStream_t st) {
     const int id = ring_pick(a.hidden, [&](int BA, int BB) { return (long)cdiv(a.C, BA) * cdiv(a.n_rows, BB); });
     return ring_dispatch(id, [&](auto c) -> hipError_t {
         constexpr int ID = decltype(c)::value;
-        using T = typename RingShape<ID, true>::Tile;
+        using T = typename RingShape<ID, RING_F16>::Tile;
         const hipError_t e = allow_lds(k_ffn_down<ID>, T::LDS_BYTES);
         if (e != hipSuccess) return e;
         const int n_at = cdiv(a.C, T::BA), n_bt = cdiv(a.n_rows, T::BB);

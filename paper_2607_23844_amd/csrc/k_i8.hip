@@ -1,10 +1,12 @@
 // Products in 8-bit integers: rows quantised with a scale each, and the product
 // of two such matrices with a fused epilogue (scales, bias, GELU, rows written
 // to their positions).
+#include "oc_attn_common.h"
 #include "oc_device.h"
+#include "oc_gemm_epi.h"
 #include "oc_launch.h"
 #include "oc_ops.h"
-#include <algorithm>
+#include "oc_ring_tile.h"
 
 namespace oc {
 
@@ -68,54 +70,113 @@ __global__ __launch_bounds__(256) void k_quant(const T *__restrict__ x, long ld,
         q[row * Kp + k] = (int8_t)(zero || k >= K ? 0 : quotient(Elem<T>::ld(x + k)));
 }
 
+// GELU in its tanh form, v / (1 + exp(-2 z)) (exp and reciprocal to 1 ulp)
 __device__ __forceinline__ float gelu_tanh(float v) {
     const float z = 0.7978845608028654f * fmaf(0.044715f * v, v * v, v);
-    return v / (1.0f + __builtin_amdgcn_exp2f(-2.8853900817779268f * z));
+    return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-2.8853900817779268f * z));
 }
 
-// A 32 x 32 tile of y per block, 16-byte steps of k through LDS, one row and
-// four columns per thread.
+// Four consecutive outputs of a row from their sums.
 template <typename T>
-__global__ __launch_bounds__(256) void k_linear_i8(LinearI8Args a) {
-    __shared__ int4 sq[32][9], sw[32][9];
-    const int Kp = (a.K + 15) & ~15, n0 = blockIdx.x * 32;
-    const long r0 = (long)blockIdx.y * 32;
-    const int tr = threadIdx.x >> 3, tc = threadIdx.x & 7;
-    int acc[4] = {};
-    for (int k0 = 0; k0 < Kp; k0 += 128) {
-        const int k = k0 + tc * 16;
-        const int4 z = make_int4(0, 0, 0, 0);
-        sq[tr][tc] = r0 + tr < a.rows && k < Kp ? *reinterpret_cast<const int4 *>(a.q + (r0 + tr) * Kp + k) : z;
-        sw[tr][tc] = n0 + tr < a.N && k < Kp ? *reinterpret_cast<const int4 *>(a.w + (long)(n0 + tr) * Kp + k) : z;
-        __syncthreads();
-        for (int c = 0; c < 8; ++c) {
-            const int4 u = sq[tr][c];
+__device__ __forceinline__ f32x4 finish4(const LinearI8Args &a, const int (&acc)[4], float sq, int n) {
+    const f32x4 sw = *reinterpret_cast<const f32x4 *>(a.sw + n);
+    f32x4 v;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int4 v = sw[tc + 8 * j][c];
-                acc[j] = __builtin_amdgcn_sdot4(u.x, v.x, acc[j], false);
-                acc[j] = __builtin_amdgcn_sdot4(u.y, v.y, acc[j], false);
-                acc[j] = __builtin_amdgcn_sdot4(u.z, v.z, acc[j], false);
-                acc[j] = __builtin_amdgcn_sdot4(u.w, v.w, acc[j], false);
-            }
+    for (int e = 0; e < 4; ++e) v[e] = (float)acc[e] * sq * sw[e];
+    if (a.bias != nullptr) {
+        if constexpr (sizeof(T) == 2) {
+            const u16x4 b = *reinterpret_cast<const u16x4 *>((const uint16_t *)a.bias + n);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += bf2f(b[e]);
+        } else {
+            v += *reinterpret_cast<const f32x4 *>((const float *)a.bias + n);
         }
-        __syncthreads();
     }
-    const long r = r0 + tr;
-    if (r >= a.rows) return;
-    const long t = a.out_idx != nullptr ? (long)a.out_idx[r] : r;
-    if (t < 0 || t >= a.n_out) return;
+    if (a.gelu) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int n = n0 + tc + 8 * j;
-        if (n >= a.N) continue;
-        float v = (float)acc[j] * a.sq[r] * a.sw[n];
-        if (a.bias != nullptr) v += Elem<T>::ld((const T *)a.bias + n);
-        if (a.gelu) v = gelu_tanh(v);
-        T *const to = (T *)a.y + t * a.ld_y + n;
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<__bf16 *>(to) = (__bf16)v;
-        else *to = v;
+        for (int e = 0; e < 4; ++e) v[e] = gelu_tanh(v[e]);
     }
+    return v;
+}
+__device__ __forceinline__ u16x4 to_bf16(f32x4 v) {
+    bf16x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (__bf16)v[e];
+    return *reinterpret_cast<u16x4 *>(&o);
+}
+
+// y row of batch row r, or -1
+__device__ __forceinline__ long out_row(const LinearI8Args &a, long r) {
+    if (r >= a.rows) return -1;
+    const long t = a.out_idx != nullptr ? (long)a.out_idx[r] : r;
+    return t >= 0 && t < a.n_out ? t : -1;
+}
+
+// ---------------------------------------------------------------------------
+// The product on ring-buffered MFMA tiles: a = weight rows, b = batch rows.
+// bf16 tiles are staged through LDS and written in 16-byte chunks of whole
+// rows; fp32 rows are stored as the accumulators hold them, four outputs at a
+// time.
+// ---------------------------------------------------------------------------
+template <int ID, typename T>
+__global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, int n_at, int n_bt) {
+    using R = typename RingShape<ID, RING_I8>::Tile;
+    constexpr int BA = R::BA, BB = R::BB;
+    extern __shared__ __align__(16) uint16_t lds[];
+    int at, bt;
+    tile_order(xcd_remap(blockIdx.x, n_at * n_bt), n_at, n_bt, at, bt);
+    const int a0 = at * BA, b0 = bt * BB;
+    const int K2 = (a.K + 15) / 16 * 8;   // pairs of elements in a row
+    typename R::RowsA ra;
+    typename R::RowsB rb;
+    ring_rows(ra, (const uint16_t *)a.w, a.N, K2, a0);
+    ring_rows(rb, (const uint16_t *)a.q, a.rows, K2, b0);
+    R t;
+    t.run(lds, ra, rb, K2);
+#pragma unroll
+    for (int j = 0; j < R::TB; ++j) {
+        const int b = R::b_of(j);
+        const float sq = a.sq[min(b0 + b, a.rows - 1)];
+        T *to = nullptr;
+        if constexpr (sizeof(T) == 4) {
+            const long o = out_row(a, b0 + b);
+            if (o >= 0) to = (T *)a.y + o * a.ld_y;
+        }
+#pragma unroll
+        for (int i = 0; i < R::TA; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int n = R::a_of(i, g);
+                if (a0 + n >= a.N) continue;
+                const int acc[4] = {t.acc[i][j][4 * g], t.acc[i][j][4 * g + 1], t.acc[i][j][4 * g + 2],
+                                    t.acc[i][j][4 * g + 3]};
+                const f32x4 v = finish4<T>(a, acc, sq, a0 + n);
+                if constexpr (sizeof(T) == 2) *reinterpret_cast<u16x4 *>(lds + b * (BA + 8) + n) = to_bf16(v);
+                else if (to != nullptr) *reinterpret_cast<f32x4 *>(to + a0 + n) = v;
+            }
+    }
+    if constexpr (sizeof(T) == 2) {
+        __syncthreads();
+        write_rows<BA, BB, R::NT>(lds, min(BA, a.N - a0), [&](int b, int c0) -> uint16_t * {
+            const long o = out_row(a, b0 + b);
+            return o >= 0 ? (uint16_t *)a.y + o * a.ld_y + a0 + c0 : nullptr;
+        });
+    }
+}
+
+template <typename T>
+hipError_t go_linear(const LinearI8Args &a, hipStream_t st) {
+    const int K2 = (int)(i8_row(a.K) / 2);
+    const int id = ring_pick(K2, [&](int BA, int BB) { return (long)cdiv(a.N, BA) * cdiv(a.rows, BB); });
+    return ring_dispatch(id, [&](auto c) -> hipError_t {
+        constexpr int ID = decltype(c)::value;
+        using R = typename RingShape<ID, RING_I8>::Tile;
+        const hipError_t e = allow_lds(k_linear_i8<ID, T>, R::LDS_BYTES);
+        if (e != hipSuccess) return e;
+        const int n_at = cdiv(a.N, R::BA), n_bt = cdiv(a.rows, R::BB);
+        launch_k(k_linear_i8<ID, T>, (unsigned)(n_at * n_bt), R::NT, R::LDS_BYTES, st, a, n_at, n_bt);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace
@@ -131,10 +192,7 @@ hipError_t launch_quant(bool bf16, const void *x, long ld, int n_src, int K, con
 
 hipError_t launch_linear_i8(const LinearI8Args &a, hipStream_t st) {
     StageScope _stage(st, "linear_i8");
-    const dim3 grid((unsigned)cdiv(a.N, 32), (unsigned)cdiv(a.rows, 32));
-    if (a.bf16) launch_k(k_linear_i8<uint16_t>, grid, 256, 0, st, a);
-    else launch_k(k_linear_i8<float>, grid, 256, 0, st, a);
-    return hipGetLastError();
+    return a.bf16 ? go_linear<uint16_t>(a, st) : go_linear<float>(a, st);
 }
 
 }  // namespace oc

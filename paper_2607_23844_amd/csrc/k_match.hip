@@ -328,7 +328,7 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_match_ring(const uint16_t 
                                                                  long sub_stride, long item_stride, int t_one,
                                                                  int t_pair, int n_at, int n_part, int total,
                                                                  unsigned long long *__restrict__ node_pack) {
-    using T = typename RingShape<ID, false>::Tile;
+    using T = typename RingShape<ID, RING_BF16>::Tile;
     constexpr int BA = T::BA, BB = T::BB, NT = T::NT, WA = BA / T::WTA;
     extern __shared__ __align__(16) uint16_t lds[];
     float *const snorm = reinterpret_cast<float *>(lds + T::RING_BYTES / 2);
@@ -707,7 +707,7 @@ static hipError_t go_ring(const Plan &p, const uint16_t *x, const float *inv, co
     const MatchPick pick = match_pick(p, mg.K, n_units, n_pairs);
     return ring_dispatch(pick.id, [&](auto c) -> hipError_t {
         constexpr int ID = decltype(c)::value;
-        using T = typename RingShape<ID, false>::Tile;
+        using T = typename RingShape<ID, RING_BF16>::Tile;
         const int n_at = cdiv(p.n_dst_max, T::BA);
         const int t_one = cdiv(p.np_src, T::BB), t_pair = cdiv(p.np + p.np_src, T::BB);
         const int total = kk * ((n_units - n_pairs) * t_one + n_pairs * t_pair) * pick.n_part;

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_proj_qkv(
     int hd, int dh, float qscale, int nw, int n_qk_at, int n_bt, int n_v_at, int n_v_bt, int n_seq, int L, int lpad,
     int zero_pad, const int32_t *__restrict__ seq_off, uint16_t *__restrict__ Q, uint16_t *__restrict__ K,
     uint16_t *__restrict__ Vt, const uint4 *__restrict__ wo, long n8, uint4 *__restrict__ wo16) {
-    using T = typename RingShape<ID, false>::Tile;
+    using T = typename RingShape<ID, RING_BF16>::Tile;
     constexpr int BA = T::BA, BB = T::BB, NT = T::NT;
     extern __shared__ __align__(16) uint16_t lds[];
     const int n_qk = n_qk_at * n_bt, total = n_qk + n_v_at * n_v_bt;
@@ -226,7 +226,7 @@ hipError_t launch_proj_qkv(const Plan &p, const RowMap &rm, const AttnArgs &a, h
     });
     return ring_dispatch(id, [&](auto c) -> hipError_t {
         constexpr int ID = decltype(c)::value;
-        using T = typename RingShape<ID, false>::Tile;
+        using T = typename RingShape<ID, RING_BF16>::Tile;
         const hipError_t e = allow_lds(k_proj_qkv<ID>, T::LDS_BYTES);
         if (e != hipSuccess) return e;
         const int n_qk_at = cdiv(nw * p.hd, T::BA), n_bt = cdiv(rm.n_rows, T::BB);
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_proj_out(
     const uint16_t *__restrict__ O, int n_rows, int hd, const uint16_t *__restrict__ wo, int C, int n_main,
     const int32_t *__restrict__ out_idx, int tF, int tN, int n_at, int n_bt, uint16_t *__restrict__ y,
     uint16_t *__restrict__ y_ctx) {
-    using T = typename RingShape<ID, true>::Tile;
+    using T = typename RingShape<ID, RING_F16>::Tile;
     constexpr int BA = T::BA, BB = T::BB;
     extern __shared__ __align__(16) uint16_t lds[];
     int at, bt;
@@ -287,7 +287,7 @@ hipError_t launch_proj_out(const Plan &p, int n_rows, const AttnArgs &a, hipStre
     const int id = ring_pick(p.hd, [&](int BA, int BB) { return (long)cdiv(p.C, BA) * cdiv(n_rows, BB); });
     return ring_dispatch(id, [&](auto c) -> hipError_t {
         constexpr int ID = decltype(c)::value;
-        using T = typename RingShape<ID, true>::Tile;
+        using T = typename RingShape<ID, RING_F16>::Tile;
         const hipError_t e = allow_lds(k_proj_out<ID>, T::LDS_BYTES);
         if (e != hipSuccess) return e;
         const int n_at = cdiv(p.C, T::BA), n_bt = cdiv(n_rows, T::BB);

@@ -26,6 +26,7 @@ namespace oc {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ uint16_t f2h_bits(float f) {
     f = fminf(fmaxf(f, -65504.f), 65504.f);

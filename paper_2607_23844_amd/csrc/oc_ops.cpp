@@ -298,6 +298,7 @@ oc_status oc_linear_i8(int32_t dtype, int32_t n_rows, int32_t K, int32_t N, cons
     if (s != OC_OK) return s;
     const size_t esz = dtype == OC_BF16 ? 2 : 4;
     if (N < 8 || N % 8 || N > (1 << 24)) return failf(OC_ERR_SHAPE, "N=%d must be a multiple of 8 in [8, 2^24]", N);
+    if ((int64_t)n_rows * N >= 1LL << 37) return failf(OC_ERR_SHAPE, "%d rows of N=%d outputs: too many", n_rows, N);
     if (act != OC_ACT_NONE && act != OC_ACT_GELU) return failf(OC_ERR_INVALID_ARG, "unknown activation %d", act);
     if (n_out < 0 || n_out >= MAX_ROWS) return failf(OC_ERR_SHAPE, "n_out=%d outside [0, 2^30)", n_out);
     if (!out_idx && n_rows > n_out) return failf(OC_ERR_SHAPE, "n_rows=%d into %d rows", n_rows, n_out);

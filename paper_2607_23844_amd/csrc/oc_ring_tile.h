@@ -1,6 +1,8 @@
 // Ring-buffered LDS-DMA MFMA tile engine for gfx950, one to three blocks per
 // compute unit: C[b][a] = sum_k A[a][k] * B[b][k] over a BA x BB tile, WA x WB waves,
-// 32x32 accumulators of v_mfma_f32_32x32x16_{bf16,f16}, K in steps of 64.
+// 32x32 accumulators of v_mfma_f32_32x32x16_{bf16,f16}, K in steps of 64; or of
+// v_mfma_i32_32x32x32_i8 (RING_I8), whose operands, fragments and LDS rows are
+// the same bytes: there every count of k below is of pairs of 8-bit elements.
 //
 // What bounds a projection here: a step moves (BA + BB) x 128 bytes from L2 to
 // LDS for BA x BB x 64 products.  Small tiles (128 x 128, two blocks per unit)
@@ -50,7 +52,9 @@ struct RingRows {
     __device__ __forceinline__ static int chunk() { return (threadIdx.x & 7) ^ ((threadIdx.x >> 4) & 7); }
 };
 
-template <int BA_, int BB_, int WA, int WB, int NST, bool F16 = false>
+enum RingType { RING_BF16, RING_F16, RING_I8 };
+
+template <int BA_, int BB_, int WA, int WB, int NST, int TYPE = RING_BF16>
 struct RingTile {
     static constexpr int BA = BA_, BB = BB_, BK = 64, NW = WA * WB, NT = NW * 64;
     static constexpr int WTA = BA / WA, WTB = BB / WB, TA = WTA / 32, TB = WTB / 32;
@@ -63,14 +67,17 @@ struct RingTile {
     static_assert(NW % 4 == 0 && WTA % 32 == 0 && WTB % 32 == 0, "wave tiles of whole accumulators");
     static_assert(CA * 8 * NW == BA && CB * 8 * NW == BB, "whole DMA instructions");
     static_assert((NST - 1) * IPT < 64 && LDS_BYTES <= 160 * 1024, "counters and LDS");
-    typedef typename std::conditional<F16, f16x8, bf16x8>::type frag;
+    typedef typename std::conditional<TYPE == RING_I8, i32x4,
+                                      typename std::conditional<TYPE == RING_F16, f16x8, bf16x8>::type>::type frag;
+    typedef typename std::conditional<TYPE == RING_I8, i32x16, f32x16>::type accu;
     typedef RingRows<CA, NW> RowsA;
     typedef RingRows<CB, NW> RowsB;
 
-    f32x16 acc[TA][TB];
+    accu acc[TA][TB];
 
-    __device__ __forceinline__ static f32x16 mma(frag a, frag b, f32x16 c) {
-        if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    __device__ __forceinline__ static accu mma(frag a, frag b, accu c) {
+        if constexpr (TYPE == RING_I8) return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0);
+        else if constexpr (TYPE == RING_F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
         else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
     template <typename R>
@@ -92,7 +99,7 @@ struct RingTile {
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
-            for (int j = 0; j < TB; ++j) acc[i][j] = f32x16{};
+            for (int j = 0; j < TB; ++j) acc[i][j] = accu{};
         const int nk = (K + BK - 1) / BK;
         // in the last step this lane's chunk may lie past K
         const uint32_t tail = (nk - 1) * BK + RowsA::chunk() * 8 < K ? 0u : RING_RECORDS;
@@ -221,8 +228,8 @@ struct RingTile {
             for (int m = 0; m < NM; ++m) {
 #pragma unroll
                 for (int r = m * NR / NM; r < (m + 1) * NR / NM; ++r) read(r, nst, nks, s ^ 1);
-                f32x16 &c = acc[m / TB][m % TB];
-                c = mma(fa[s][m / TB], fb[s][m % TB], decltype(fresh)::value ? f32x16{} : c);
+                accu &c = acc[m / TB][m % TB];
+                c = mma(fa[s][m / TB], fb[s][m % TB], decltype(fresh)::value ? accu{} : c);
                 if (dst != nullptr && go) {
 #pragma unroll
                     for (int d = m * IPT / NM; d < (m + 1) * IPT / NM; ++d) issue(d, dst, oob);
@@ -327,19 +334,19 @@ constexpr RingShapeCost RING_SHAPES[] = {
     {64, 64, 3, 1.75f, {0.213f, 0.276f, 0.503f}}, {128, 64, 2, 2.26f, {0.277f, 0.537f}},
 };
 constexpr int N_RING_SHAPES = sizeof(RING_SHAPES) / sizeof(RING_SHAPES[0]);
-template <int ID, bool F16> struct RingShape;
-template <bool F16> struct RingShape<0, F16> { using Tile = RingTile<256, 256, 4, 2, 2, F16>; };
-template <bool F16> struct RingShape<1, F16> { using Tile = RingTile<256, 192, 4, 2, 2, F16>; };
-template <bool F16> struct RingShape<2, F16> { using Tile = RingTile<256, 128, 4, 2, 3, F16>; };
-template <bool F16> struct RingShape<3, F16> { using Tile = RingTile<128, 192, 2, 2, 3, F16>; };
-template <bool F16> struct RingShape<4, F16> { using Tile = RingTile<96, 128, 1, 4, 5, F16>; };
-template <bool F16> struct RingShape<5, F16> { using Tile = RingTile<128, 128, 2, 2, 2, F16>; };
-template <bool F16> struct RingShape<6, F16> { using Tile = RingTile<128, 192, 2, 2, 2, F16>; };
-template <bool F16> struct RingShape<7, F16> { using Tile = RingTile<160, 128, 1, 4, 2, F16>; };
-template <bool F16> struct RingShape<8, F16> { using Tile = RingTile<64, 64, 2, 2, 3, F16>; };
-template <bool F16> struct RingShape<9, F16> { using Tile = RingTile<128, 64, 2, 2, 3, F16>; };
-template <int ID> constexpr int RING_THREADS = RingShape<ID, false>::Tile::NT;
-template <int ID> constexpr size_t RING_LDS = RingShape<ID, false>::Tile::RING_BYTES;
+template <int ID, int TYPE> struct RingShape;
+template <int TYPE> struct RingShape<0, TYPE> { using Tile = RingTile<256, 256, 4, 2, 2, TYPE>; };
+template <int TYPE> struct RingShape<1, TYPE> { using Tile = RingTile<256, 192, 4, 2, 2, TYPE>; };
+template <int TYPE> struct RingShape<2, TYPE> { using Tile = RingTile<256, 128, 4, 2, 3, TYPE>; };
+template <int TYPE> struct RingShape<3, TYPE> { using Tile = RingTile<128, 192, 2, 2, 3, TYPE>; };
+template <int TYPE> struct RingShape<4, TYPE> { using Tile = RingTile<96, 128, 1, 4, 5, TYPE>; };
+template <int TYPE> struct RingShape<5, TYPE> { using Tile = RingTile<128, 128, 2, 2, 2, TYPE>; };
+template <int TYPE> struct RingShape<6, TYPE> { using Tile = RingTile<128, 192, 2, 2, 2, TYPE>; };
+template <int TYPE> struct RingShape<7, TYPE> { using Tile = RingTile<160, 128, 1, 4, 2, TYPE>; };
+template <int TYPE> struct RingShape<8, TYPE> { using Tile = RingTile<64, 64, 2, 2, 3, TYPE>; };
+template <int TYPE> struct RingShape<9, TYPE> { using Tile = RingTile<128, 64, 2, 2, 3, TYPE>; };
+template <int ID> constexpr int RING_THREADS = RingShape<ID, RING_BF16>::Tile::NT;
+template <int ID> constexpr size_t RING_LDS = RingShape<ID, RING_BF16>::Tile::RING_BYTES;
 
 // us for `blocks` blocks of nk steps each, with `epi` us of other work per block
 inline float ring_cost(const RingShapeCost &c, int nk, long blocks, float epi = 0.f) {
