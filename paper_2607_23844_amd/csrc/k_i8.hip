@@ -45,29 +45,115 @@ template <> struct QuotientOf<uint16_t> { typedef Quotient16 type; };
 
 constexpr uint32_t INF_BITS = 0x7F800000u;   // magnitudes from here on: infinities and NaNs
 
+// A row of 8 elements per chunk, kept as it was read.
+template <typename T> struct Raw8 { uint4 v[sizeof(T) / 2]; };
 template <typename T>
+__device__ __forceinline__ Raw8<T> raw8(const T *p) {
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.v[i] = reinterpret_cast<const uint4 *>(p)[i];
+    return r;
+}
+__device__ __forceinline__ void widen(const Raw8<uint16_t> &r, float (&v)[8]) {
+    const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void widen(const Raw8<float> &r, float (&v)[8]) {
+    const uint32_t w[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+}
+
+// A row by TPR threads (a wave, or the block of 256), read once: CH chunks of
+// 8 elements per thread stay in registers between the maximum and the
+// quotients.  CH = 0: rows too long for that, read twice.
+template <typename T, int TPR, int CH>
 __global__ __launch_bounds__(256) void k_quant(const T *__restrict__ x, long ld, int n_src, int K,
                                                const int32_t *__restrict__ idx, int rows, int8_t *__restrict__ q,
                                                float *__restrict__ scale) {
+    constexpr int N = CH > 0 ? CH : 1;
     __shared__ uint32_t red[4];
-    const long row = folded_block();
+    const int lane = threadIdx.x % TPR;
+    const long row = (long)folded_block() * (256 / TPR) + threadIdx.x / TPR;
     if (row >= rows) return;
     const long src = idx != nullptr ? (long)idx[row] : row;
     if (src < 0 || src >= n_src) return;
     x += src * ld;
     uint32_t m = 0;
-    for (int k = threadIdx.x; k < K; k += 256) m = max(m, __float_as_uint(Elem<T>::ld(x + k)) & 0x7FFFFFFFu);
-    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, WAVE));
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-    __syncthreads();
-    m = max(max(red[0], red[1]), max(red[2], red[3]));
+    auto widest = [&](const Raw8<T> &r) {
+        float v[8];
+        widen(r, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+    };
+    Raw8<T> keep[N];
+    if constexpr (CH > 0) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int k = (lane + i * TPR) * 8;
+            if (k < K) keep[i] = raw8(x + k);
+        }
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+            if ((lane + i * TPR) * 8 < K) widest(keep[i]);
+    } else {
+        for (int k = lane * 8; k < K; k += TPR * 8) widest(raw8(x + k));
+    }
+    m = wave_all_max(m);
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+        __syncthreads();
+        m = max(max(red[0], red[1]), max(red[2], red[3]));
+    }
     const float top = __uint_as_float(m);
-    if (threadIdx.x == 0) scale[row] = m >= INF_BITS ? __uint_as_float(0x7FC00000u) : top / 127.f;
+    if (lane == 0) scale[row] = m >= INF_BITS ? __uint_as_float(0x7FC00000u) : top / 127.f;
     const bool zero = m == 0 || m >= INF_BITS;
     const typename QuotientOf<T>::type quotient(zero ? 1.f : top);
     const int Kp = (K + 15) & ~15;
-    for (int k = threadIdx.x; k < Kp; k += 256)
-        q[row * Kp + k] = (int8_t)(zero || k >= K ? 0 : quotient(Elem<T>::ld(x + k)));
+    q += row * Kp;
+    auto write = [&](int k, const Raw8<T> &r) {
+        float v[8];
+        widen(r, v);
+        uint32_t w[2] = {0, 0};
+        if (!zero) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e / 4] |= (uint32_t)(quotient(v[e]) & 0xFF) << (e % 4 * 8);
+        }
+        *reinterpret_cast<uint2 *>(q + k) = make_uint2(w[0], w[1]);
+    };
+    if constexpr (CH > 0) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int k = (lane + i * TPR) * 8;
+            if (k < K) write(k, keep[i]);
+        }
+    } else {
+        for (int k = lane * 8; k < K; k += TPR * 8) write(k, raw8(x + k));
+    }
+    if (Kp > K && lane == 0) *reinterpret_cast<uint2 *>(q + K) = make_uint2(0, 0);   // (K is a multiple of 8)
+}
+
+template <typename T>
+hipError_t go_quant(const T *x, long ld, int n_src, int K, const int *idx, int rows, int8_t *q, float *scale,
+                    hipStream_t st) {
+    auto go = [&](auto kern, int per_block) {
+        launch_k(kern, folded_grid((rows + per_block - 1) / per_block, 256), 256, 0, st, x, ld, n_src, K, idx, rows, q,
+                 scale);
+        return hipGetLastError();
+    };
+    // a wave for a short row where there are rows for all units, else the block
+    const int c = cdiv(K, 8);
+    if (c <= 256 && rows >= 2 * N_CUS) {
+        if (c <= 64) return go(k_quant<T, 64, 1>, 4);
+        return c <= 128 ? go(k_quant<T, 64, 2>, 4) : go(k_quant<T, 64, 4>, 4);
+    }
+    if (c <= 256) return go(k_quant<T, 256, 1>, 1);
+    if (c <= 512) return go(k_quant<T, 256, 2>, 1);
+    return c <= 1024 ? go(k_quant<T, 256, 4>, 1) : go(k_quant<T, 256, 0>, 1);
 }
 
 // GELU in its tanh form, v / (1 + exp(-2 z)) (exp and reciprocal to 1 ulp)
@@ -164,8 +250,82 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, 
     }
 }
 
+// ---------------------------------------------------------------------------
+// The product of few rows: bound by the weights' way from HBM, so a block takes
+// 16 weight rows and all its waves share out their K (the ring's tiles would be
+// N / 64 blocks of one after another 128 bytes).  v_mfma_i32_16x16x64_i8, a =
+// weights, b = up to 16 RT batch rows; any order of k will do as long as both
+// operands agree, so a lane takes 64 consecutive bytes of its row for four
+// MFMAs.  The waves' sums are added in LDS (integers: in any order).
+// ---------------------------------------------------------------------------
+template <typename T, int RT>
+__global__ __launch_bounds__(1024) void k_linear_i8_thin(LinearI8Args a) {
+    extern __shared__ __align__(16) int part[];   // [wave][RT][16 batch rows][16 + 4 outputs]
+    constexpr int LD = 20;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
+    const int lr = lane & 15, lg = lane >> 4, n0 = blockIdx.x * 16;
+    const int Kp = (a.K + 15) & ~15;
+    const int8_t *w = a.w + (long)min(n0 + lr, a.N - 1) * Kp;
+    const int8_t *q[RT];
+    i32x4 acc[RT];
+    const i32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        q[t] = a.q + (long)min(t * 16 + lr, a.rows - 1) * Kp;
+        acc[t] = zero;
+    }
+    for (int k0 = wave * 256; k0 < Kp; k0 += nw * 256) {
+        i32x4 fw[4], fq[RT][4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int k = k0 + lg * 64 + s * 16;
+            fw[s] = k < Kp ? *reinterpret_cast<const i32x4 *>(w + k) : zero;
+#pragma unroll
+            for (int t = 0; t < RT; ++t) fq[t][s] = k < Kp ? *reinterpret_cast<const i32x4 *>(q[t] + k) : zero;
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+                acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[s], fq[t][s], acc[t], 0, 0, 0);
+    }
+    // lane: batch row lr, outputs 4 lg .. 4 lg + 3
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+        *reinterpret_cast<i32x4 *>(part + ((wave * RT + t) * 16 + lr) * LD + lg * 4) = acc[t];
+    __syncthreads();
+    for (int i = threadIdx.x; i < RT * 64; i += blockDim.x) {
+        const int r = i >> 2, n = (i & 3) * 4;
+        const long o = out_row(a, r);
+        if (o < 0 || n0 + n >= a.N) continue;
+        i32x4 s = zero;
+        for (int v = 0; v < nw; ++v) s += *reinterpret_cast<const i32x4 *>(part + (v * RT * 16 + r) * LD + n);
+        const int sum[4] = {s[0], s[1], s[2], s[3]};
+        const f32x4 f = finish4<T>(a, sum, a.sq[r], n0 + n);
+        T *const to = (T *)a.y + o * a.ld_y + n0 + n;
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<u16x4 *>(to) = to_bf16(f);
+        else *reinterpret_cast<f32x4 *>(to) = f;
+    }
+}
+
+template <typename T, int RT>
+hipError_t go_thin(const LinearI8Args &a, hipStream_t st) {
+    // waves: a pass of 256 bytes of k each, while a unit has fewer than eight
+    const int blocks = cdiv(a.N, 16), passes = cdiv(a.K, 256);
+    int nw = 4;
+    while (nw < 16 && nw < passes && (long)blocks * nw < 8L * N_CUS) nw *= 2;
+    const size_t lds = (size_t)nw * RT * 16 * 20 * 4;
+    const hipError_t e = raise_lds_limit((const void *)k_linear_i8_thin<T, RT>, lds);
+    if (e != hipSuccess) return e;
+    launch_k(k_linear_i8_thin<T, RT>, (unsigned)blocks, nw * 64, lds, st, a);
+    return hipGetLastError();
+}
+
 template <typename T>
 hipError_t go_linear(const LinearI8Args &a, hipStream_t st) {
+    if (a.rows <= 16) return go_thin<T, 1>(a, st);
+    if (a.rows <= 32) return go_thin<T, 2>(a, st);
+    if (a.rows <= 64) return go_thin<T, 4>(a, st);
     const int K2 = (int)(i8_row(a.K) / 2);
     const int id = ring_pick(K2, [&](int BA, int BB) { return (long)cdiv(a.N, BA) * cdiv(a.rows, BB); });
     return ring_dispatch(id, [&](auto c) -> hipError_t {
@@ -184,10 +344,8 @@ hipError_t go_linear(const LinearI8Args &a, hipStream_t st) {
 hipError_t launch_quant(bool bf16, const void *x, long ld, int n_src, int K, const int *idx, int rows, int8_t *q,
                         float *scale, hipStream_t st) {
     StageScope _stage(st, "quant_rows");
-    const dim3 grid = folded_grid(rows, 256);
-    if (bf16) launch_k(k_quant<uint16_t>, grid, 256, 0, st, (const uint16_t *)x, ld, n_src, K, idx, rows, q, scale);
-    else launch_k(k_quant<float>, grid, 256, 0, st, (const float *)x, ld, n_src, K, idx, rows, q, scale);
-    return hipGetLastError();
+    return bf16 ? go_quant((const uint16_t *)x, ld, n_src, K, idx, rows, q, scale, st)
+                : go_quant((const float *)x, ld, n_src, K, idx, rows, q, scale, st);
 }
 
 hipError_t launch_linear_i8(const LinearI8Args &a, hipStream_t st) {

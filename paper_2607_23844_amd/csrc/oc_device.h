@@ -60,6 +60,44 @@ __device__ __forceinline__ float wave_max(float v) {
     return v;
 }
 
+// Sum and maximum over a wave in every lane: within rows of 16 lanes by DPP
+// operands, across them by the swaps of rows and halves, no LDS.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_mov(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xF, 0xF, true);
+}
+// lanes' values from 16 (32) lanes away: the pair of both in each lane
+__device__ __forceinline__ void swap16(uint32_t v, uint32_t &a, uint32_t &b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    a = r[0];
+    b = r[1];
+}
+__device__ __forceinline__ void swap32(uint32_t v, uint32_t &a, uint32_t &b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    a = r[0];
+    b = r[1];
+}
+template <typename Op>
+__device__ __forceinline__ uint32_t wave_all(uint32_t v, Op op) {
+    v = op(v, dpp_mov<0xB1>(v));    // lane ^ 1
+    v = op(v, dpp_mov<0x4E>(v));    // lane ^ 2
+    v = op(v, dpp_mov<0x141>(v));   // mirrored in 8: the other four
+    v = op(v, dpp_mov<0x140>(v));   // mirrored in 16: the other eight
+    uint32_t a, b;
+    swap16(v, a, b);
+    v = op(a, b);
+    swap32(v, a, b);
+    return op(a, b);
+}
+__device__ __forceinline__ float wave_all_sum(float v) {
+    return __uint_as_float(wave_all(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
+__device__ __forceinline__ uint32_t wave_all_max(uint32_t v) {
+    return wave_all(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+
 // (value, index) arg-max merge: larger value wins, smaller index on ties.
 __device__ __forceinline__ void argmax_merge(float &v, int &i, float v2, int i2) {
     if (v2 > v || (v2 == v && (unsigned)i2 < (unsigned)i)) { v = v2; i = i2; }
