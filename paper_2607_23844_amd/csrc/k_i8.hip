@@ -254,9 +254,8 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, 
 // The product of few rows: bound by the weights' way from HBM, so a block takes
 // 16 weight rows and all its waves share out their K (the ring's tiles would be
 // N / 64 blocks of one after another 128 bytes).  v_mfma_i32_16x16x64_i8, a =
-// weights, b = up to 16 RT batch rows; any order of k will do as long as both
-// operands agree, so a lane takes 64 consecutive bytes of its row for four
-// MFMAs.  The waves' sums are added in LDS (integers: in any order).
+// weights, b = up to 16 RT batch rows, four of them from one round of loads.
+// The waves' sums are added in LDS (integers: in any order).
 // ---------------------------------------------------------------------------
 template <typename T, int RT>
 __global__ __launch_bounds__(1024) void k_linear_i8_thin(LinearI8Args a) {
@@ -278,7 +277,7 @@ __global__ __launch_bounds__(1024) void k_linear_i8_thin(LinearI8Args a) {
         i32x4 fw[4], fq[RT][4];
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const int k = k0 + lg * 64 + s * 16;
+            const int k = k0 + s * 64 + lg * 16;
             fw[s] = k < Kp ? *reinterpret_cast<const i32x4 *>(w + k) : zero;
 #pragma unroll
             for (int t = 0; t < RT; ++t) fq[t][s] = k < Kp ? *reinterpret_cast<const i32x4 *>(q[t] + k) : zero;
@@ -310,10 +309,8 @@ __global__ __launch_bounds__(1024) void k_linear_i8_thin(LinearI8Args a) {
 
 template <typename T, int RT>
 hipError_t go_thin(const LinearI8Args &a, hipStream_t st) {
-    // waves: a pass of 256 bytes of k each, while a unit has fewer than eight
-    const int blocks = cdiv(a.N, 16), passes = cdiv(a.K, 256);
-    int nw = 4;
-    while (nw < 16 && nw < passes && (long)blocks * nw < 8L * N_CUS) nw *= 2;
+    // waves: one pass of 256 bytes of k each, or as few as 16 waves need
+    const int blocks = cdiv(a.N, 16), passes = cdiv(a.K, 256), nw = cdiv(passes, cdiv(passes, 16));
     const size_t lds = (size_t)nw * RT * 16 * 20 * 4;
     const hipError_t e = raise_lds_limit((const void *)k_linear_i8_thin<T, RT>, lds);
     if (e != hipSuccess) return e;
@@ -323,9 +320,11 @@ hipError_t go_thin(const LinearI8Args &a, hipStream_t st) {
 
 template <typename T>
 hipError_t go_linear(const LinearI8Args &a, hipStream_t st) {
+    // Up to 16 rows: 3.9 us against the ring's 6.7 for one row of K = N = 1536, 6.3 against 8.5 at N =
+    // 9216.  Up to 32 while the ring's tiles of 64 outputs are few: 32 rows, K = 1536, N = 1536 5.2
+    // against 6.8, N = 4608 7.3 against 7.0 (every block reads all rows from L2).
     if (a.rows <= 16) return go_thin<T, 1>(a, st);
-    if (a.rows <= 32) return go_thin<T, 2>(a, st);
-    if (a.rows <= 64) return go_thin<T, 4>(a, st);
+    if (a.rows <= 32 && a.N <= 4096) return go_thin<T, 2>(a, st);
     const int K2 = (int)(i8_row(a.K) / 2);
     const int id = ring_pick(K2, [&](int BA, int BB) { return (long)cdiv(a.N, BA) * cdiv(a.rows, BB); });
     return ring_dispatch(id, [&](auto c) -> hipError_t {

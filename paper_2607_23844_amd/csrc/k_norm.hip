@@ -11,7 +11,9 @@
 #include "oc_device.h"
 #include "oc_launch.h"
 #include "oc_ops.h"
+#include "oc_attn_common.h"
 #include <algorithm>
+#include <type_traits>
 
 namespace oc {
 
@@ -63,6 +65,143 @@ __device__ __forceinline__ float block_sum(float v, float *red) {
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
+// ---------------------------------------------------------------------------
+// Rows that stay in registers.  A team (a wave, or the block of 256 threads)
+// holds a row in CH chunks of 8 channels per thread, so x, y, dh and dn are
+// read once, whatever the number of means over them.
+// ---------------------------------------------------------------------------
+template <int TPR>
+struct Team {
+    static constexpr int PER_BLOCK = 256 / TPR;
+    static __device__ __forceinline__ int lane() { return threadIdx.x % TPR; }
+    static __device__ __forceinline__ int id() { return threadIdx.x / TPR; }
+    // sums over the team, in every thread (red: 8 floats; not used by a wave)
+    static __device__ __forceinline__ void sum2(float &a, float &b, float *red) {
+        a = wave_all_sum(a);
+        b = wave_all_sum(b);
+        if constexpr (TPR > 64) {
+            __syncthreads();   // red may still be read
+            if ((threadIdx.x & 63) == 0) {
+                red[threadIdx.x >> 6] = a;
+                red[4 + (threadIdx.x >> 6)] = b;
+            }
+            __syncthreads();
+            a = (red[0] + red[1]) + (red[2] + red[3]);
+            b = (red[4] + red[5]) + (red[6] + red[7]);
+        }
+    }
+    static __device__ __forceinline__ float sum(float a, float *red) {
+        float b = 0.f;
+        if constexpr (TPR > 64) sum2(a, b, red);
+        else a = wave_all_sum(a);
+        return a;
+    }
+};
+
+template <typename T, int TPR, int CH>
+struct RegRow {
+    typedef float Vals[CH][8];
+    int C, c0;   // channels, this thread's first
+    __device__ __forceinline__ explicit RegRow(int channels) : C(channels), c0(Team<TPR>::lane() * 8) {}
+    __device__ __forceinline__ int at(int i) const { return c0 + i * TPR * 8; }
+    __device__ __forceinline__ bool in(int i) const { return at(i) < C; }
+    // channels past C: other
+    __device__ __forceinline__ void load(const T *p, Vals &v, float other) const {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            if (p != nullptr && in(i)) {
+                load8(p + at(i), v[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = other;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(T *p, const Vals &v) const {
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+            if (in(i)) store8(p + at(i), v[i]);
+    }
+    // v -> (v - mean) rstd; values past C stay 0
+    __device__ __forceinline__ float normalise(int kind, float eps, Vals &v, float *red) const {
+        if (kind == 0) return 1.f;
+        float mean = 0.f, s = 0.f;
+        if (kind == NORM_LAYER) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s += v[i][e];
+            mean = Team<TPR>::sum(s, red) / (float)C;
+            s = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (kind == NORM_LAYER) v[i][e] = in(i) ? v[i][e] - mean : 0.f;
+                s = fmaf(v[i][e], v[i][e], s);
+            }
+        const float rstd = 1.f / sqrtf(Team<TPR>::sum(s, red) / (float)C + eps);
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] *= rstd;
+        return rstd;
+    }
+};
+
+// Bound by the rows' way through HBM: x, y, h and n once each.  (The vectors
+// come from the caches.)
+template <typename T, int TPR, int CH>
+__global__ __launch_bounds__(256) void k_norm_gate(NormArgs a, T *h, T *n) {
+    typedef RegRow<T, TPR, CH> Row;
+    __shared__ float red[8];
+    const long row = (long)folded_block() * Team<TPR>::PER_BLOCK + Team<TPR>::id();
+    if (row >= a.rows) return;
+    const Row r(a.C);
+    const long at = row * a.C, mod = row / a.rows_per_mod * a.ld;
+    typename Row::Vals v, z, w, b;
+    r.load((const T *)a.x + at, v, 0.f);
+    if (a.y != nullptr) {
+        r.load((const T *)a.y + at, z, 0.f);
+        r.normalise(a.post, a.post_eps, z, red);
+        if (a.post_w != nullptr || a.post_b != nullptr) {
+            r.load((const T *)a.post_w, w, 1.f);
+            r.load((const T *)a.post_b, b, 0.f);
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[i][e] = r.in(i) ? fmaf(z[i][e], w[i][e], b[i][e]) : 0.f;
+        }
+        r.load(a.gate != nullptr ? (const T *)a.gate + mod : nullptr, w, 1.f);
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = fmaf(w[i][e], z[i][e], a.res_scale * v[i][e]);
+        if (h != nullptr) r.store(h + at, v);
+    }
+    if (n == nullptr) return;
+    r.normalise(a.pre, a.pre_eps, v, red);
+    if (a.pre_w != nullptr || a.pre_b != nullptr) {
+        r.load((const T *)a.pre_w, w, 1.f);
+        r.load((const T *)a.pre_b, b, 0.f);
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e], w[i][e], b[i][e]);
+    }
+    if (a.scale != nullptr || a.shift != nullptr) {
+        r.load(a.scale != nullptr ? (const T *)a.scale + mod : nullptr, w, 0.f);
+        r.load(a.shift != nullptr ? (const T *)a.shift + mod : nullptr, b, 0.f);
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e], 1.f + w[i][e], b[i][e]);
+    }
+    r.store(n + at, v);
+}
+
+// Rows too long for that: read again for every pass over them.
 struct Stats { float mean, rstd; };
 
 // One row, its chunks of 8 channels spread over the block.
@@ -125,7 +264,7 @@ struct NormRow {
 };
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm_gate(NormArgs a, T *h, T *n) {
+__global__ __launch_bounds__(256) void k_norm_gate_wide(NormArgs a, T *h, T *n) {
     __shared__ float red[4];
     const long row = folded_block();
     if (row >= a.rows) return;
@@ -358,12 +497,43 @@ hipError_t launch_zero(float *p, int n, hipStream_t st) {
     return hipGetLastError();
 }
 
+// f(threads per row, chunks of 8 channels per thread) for a row of C channels;
+// (256, 0): too long for registers.  A wave for a row of up to 2048 where there
+// are rows for all units, else the block.
+template <typename F>
+static hipError_t norm_shape(int rows, int C, F f) {
+    using std::integral_constant;
+    const int c = cdiv(C, 8);
+    if (c <= 256 && rows >= 4 * N_CUS) {
+        constexpr integral_constant<int, 64> wave{};
+        switch (cdiv(c, 64)) {
+            case 1: return f(wave, integral_constant<int, 1>{});
+            case 2: return f(wave, integral_constant<int, 2>{});
+            case 3: return f(wave, integral_constant<int, 3>{});
+            default: return f(wave, integral_constant<int, 4>{});
+        }
+    }
+    constexpr integral_constant<int, 256> block{};
+    if (c <= 256) return f(block, integral_constant<int, 1>{});
+    if (c <= 512) return f(block, integral_constant<int, 2>{});
+    return c <= 1024 ? f(block, integral_constant<int, 4>{}) : f(block, integral_constant<int, 0>{});
+}
+
+template <typename T>
+static hipError_t go_norm_gate(const NormArgs &a, T *h, T *n, hipStream_t st) {
+    return norm_shape(a.rows, a.C, [&](auto tpr, auto ch) -> hipError_t {
+        constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
+        if constexpr (CH == 0)
+            launch_k(k_norm_gate_wide<T>, folded_grid(a.rows, 256), 256, 0, st, a, h, n);
+        else
+            launch_k(k_norm_gate<T, TPR, CH>, folded_grid(((long)a.rows * TPR + 255) / 256, 256), 256, 0, st, a, h, n);
+        return hipGetLastError();
+    });
+}
+
 hipError_t launch_norm_gate(const NormArgs &a, void *h, void *n, hipStream_t st) {
     StageScope _stage(st, "norm_gate");
-    const dim3 grid = folded_grid(a.rows, 256);
-    if (a.bf16) launch_k(k_norm_gate<uint16_t>, grid, 256, 0, st, a, (uint16_t *)h, (uint16_t *)n);
-    else launch_k(k_norm_gate<float>, grid, 256, 0, st, a, (float *)h, (float *)n);
-    return hipGetLastError();
+    return a.bf16 ? go_norm_gate(a, (uint16_t *)h, (uint16_t *)n, st) : go_norm_gate(a, (float *)h, (float *)n, st);
 }
 
 size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod) {
