@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void k_quant(const T *__restrict__ x, long ld,
     } else {
         for (int k = lane * 8; k < K; k += TPR * 8) widest(raw8(x + k));
     }
-    m = wave_all_max(m);
+    m = lanes_max(m);
     if constexpr (TPR > 64) {
         if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
         __syncthreads();

@@ -66,7 +66,7 @@ __device__ __forceinline__ float block_sum(float v, float *red) {
 }
 
 // ---------------------------------------------------------------------------
-// Rows that stay in registers.  A team (a wave, or the block of 256 threads)
+// Rows that stay in registers.  A team (16, 32 or 64 lanes, or the block of 256)
 // holds a row in CH chunks of 8 channels per thread, so x, y, dh and dn are
 // read once, whatever the number of means over them.
 // ---------------------------------------------------------------------------
@@ -75,10 +75,10 @@ struct Team {
     static constexpr int PER_BLOCK = 256 / TPR;
     static __device__ __forceinline__ int lane() { return threadIdx.x % TPR; }
     static __device__ __forceinline__ int id() { return threadIdx.x / TPR; }
-    // sums over the team, in every thread (red: 8 floats; not used by a wave)
+    // sums over the team, in every thread (red: 8 floats, for the block)
     static __device__ __forceinline__ void sum2(float &a, float &b, float *red) {
-        a = wave_all_sum(a);
-        b = wave_all_sum(b);
+        a = lanes_sum<(TPR < 64 ? TPR : 64)>(a);
+        b = lanes_sum<(TPR < 64 ? TPR : 64)>(b);
         if constexpr (TPR > 64) {
             __syncthreads();   // red may still be read
             if ((threadIdx.x & 63) == 0) {
@@ -93,7 +93,7 @@ struct Team {
     static __device__ __forceinline__ float sum(float a, float *red) {
         float b = 0.f;
         if constexpr (TPR > 64) sum2(a, b, red);
-        else a = wave_all_sum(a);
+        else a = lanes_sum<TPR>(a);
         return a;
     }
 };
@@ -199,6 +199,204 @@ __global__ __launch_bounds__(256) void k_norm_gate(NormArgs a, T *h, T *n) {
             for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e], 1.f + w[i][e], b[i][e]);
     }
     r.store(n + at, v);
+}
+
+enum { Q_GATE, Q_SCALE, Q_SHIFT, Q_POSTW, Q_POSTB, Q_PREW, Q_PREB, N_Q };
+constexpr int ACC_MODS = 1, ACC_VECS = 2;   // sums that a gradient call keeps
+
+// Work of the gradients: item i is rows [start, end) of one modulation row,
+// group i / per_group, split into per_group items.
+struct GradItems {
+    float *out[N_Q];        // results, or NULL
+    float *slots;           // [3][n_items][C], per_group > 1
+    float *sums;            // [4][blocks][C]
+    int part, per_group, n_items;   // rows of an item
+    int alone;              // a team takes an item by itself (else the block's teams share it)
+};
+
+// The gradients of rows in registers: x, y, dh, dn are read and dx, dy written
+// once, which bounds it.  Sums over rows stay in registers over an item (the
+// modulation's) or all items of the block (the norms' vectors); the block's
+// teams are added in LDS, blocks by k_norm_grad_join, in the order of their
+// numbers.
+template <typename T, int TPR, int CH, int ACC>
+__global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, const T *dn, T *dx, T *dy, GradItems g) {
+    typedef RegRow<T, TPR, CH> Row;
+    typedef typename Row::Vals Vals;
+    constexpr int TEAMS = Team<TPR>::PER_BLOCK;
+    constexpr int NM = ACC & ACC_MODS ? 3 : 0, NV = ACC & ACC_VECS ? 4 : 0;
+    extern __shared__ __align__(16) float comb[];   // [team][TPR * CH * 8], TEAMS > 1
+    __shared__ float red[8];
+    const Row r(a.C);
+    const int team = Team<TPR>::id();
+    Vals q[NM + NV > 0 ? NM + NV : 1];
+#pragma unroll
+    for (int k = 0; k < NM + NV; ++k)
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[k][i][e] = 0.f;
+    // the block's sum of v to `to`
+    auto flush = [&](Vals &v, float *to, bool shared) {
+        if (TEAMS == 1 || !shared) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+                if (r.in(i)) store8(to + r.at(i), v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) store8(comb + team * (TPR * CH * 8) + r.at(i), v[i]);
+            __syncthreads();
+            for (int c = threadIdx.x * 4; c < a.C; c += 1024) {
+                f32x4 s = *reinterpret_cast<const f32x4 *>(comb + c);
+#pragma unroll
+                for (int t = 1; t < TEAMS; ++t) s += *reinterpret_cast<const f32x4 *>(comb + t * (TPR * CH * 8) + c);
+                *reinterpret_cast<f32x4 *>(to + c) = s;
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+    };
+    const int first = g.alone ? (int)blockIdx.x * TEAMS + team : (int)blockIdx.x;
+    const int items = (int)gridDim.x * (g.alone ? TEAMS : 1);
+    for (int item = first; item < g.n_items; item += items) {
+        const int group = item / g.per_group;
+        const long start = (long)group * a.rows_per_mod + (long)(item - group * g.per_group) * g.part;
+        const long stop = min(min(start + g.part, (long)(group + 1) * a.rows_per_mod), (long)a.rows);
+        const long mod = group * a.ld;
+        for (long row = start + (g.alone ? 0 : team); row < stop; row += g.alone ? 1 : TEAMS) {
+            const long at = row * a.C;
+            Vals u, v, t, H, w, b;
+            r.load((const T *)a.x + at, u, 0.f);
+            r.load(dn != nullptr ? dn + at : nullptr, t, 0.f);
+            float ry = 1.f;
+            if (a.y != nullptr) {
+                r.load((const T *)a.y + at, v, 0.f);
+                ry = r.normalise(a.post, a.post_eps, v, red);
+                Vals gt;
+                r.load((const T *)a.post_w, w, 1.f);
+                r.load((const T *)a.post_b, b, 0.f);
+                r.load(a.gate != nullptr ? (const T *)a.gate + mod : nullptr, gt, 1.f);
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        u[i][e] = fmaf(gt[i][e], fmaf(v[i][e], w[i][e], b[i][e]), a.res_scale * u[i][e]);
+            }
+            r.load(dh != nullptr ? dh + at : nullptr, H, 0.f);
+            const float rh = r.normalise(a.pre, a.pre_eps, u, red);
+            float s1 = 0.f, s2 = 0.f;
+            {
+                Vals s;
+                r.load((const T *)a.pre_w, w, 1.f);
+                r.load((const T *)a.pre_b, b, 0.f);
+                r.load(a.scale != nullptr ? (const T *)a.scale + mod : nullptr, s, 0.f);
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float d = t[i][e], da = d * (1.f + s[i][e]), ue = u[i][e];
+                        if constexpr (NM > 0) {
+                            q[Q_SCALE][i][e] = fmaf(d, fmaf(ue, w[i][e], b[i][e]), q[Q_SCALE][i][e]);
+                            q[Q_SHIFT][i][e] += d;
+                        }
+                        if constexpr (NV > 0) {
+                            q[NM + Q_PREW - 3][i][e] = fmaf(da, ue, q[NM + Q_PREW - 3][i][e]);
+                            q[NM + Q_PREB - 3][i][e] += da;
+                        }
+                        const float dv = da * w[i][e];
+                        t[i][e] = dv;
+                        s1 += dv;
+                        s2 = fmaf(dv, ue, s2);
+                    }
+            }
+            float m1 = 0.f, m2 = 0.f;
+            if (a.pre != 0) {
+                Team<TPR>::sum2(s1, s2, red);
+                m1 = a.pre == NORM_LAYER ? s1 / (float)a.C : 0.f;
+                m2 = s2 / (float)a.C;
+            }
+            const float rs = a.y != nullptr ? a.res_scale : 1.f;
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    // (past C: not the means' share)
+                    H[i][e] = r.in(i) ? fmaf(rh, t[i][e] - m1 - u[i][e] * m2, H[i][e]) : 0.f;
+                    u[i][e] = rs * H[i][e];
+                }
+            if (dx != nullptr) r.store(dx + at, u);
+            if (a.y == nullptr) continue;
+            s1 = s2 = 0.f;
+            {
+                Vals gt;
+                r.load((const T *)a.post_w, w, 1.f);
+                r.load((const T *)a.post_b, b, 0.f);
+                r.load(a.gate != nullptr ? (const T *)a.gate + mod : nullptr, gt, 1.f);
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float ve = v[i][e], he = H[i][e], dz = he * gt[i][e];
+                        if constexpr (NM > 0)
+                            q[Q_GATE][i][e] = fmaf(he, fmaf(ve, w[i][e], b[i][e]), q[Q_GATE][i][e]);
+                        if constexpr (NV > 0) {
+                            q[NM + Q_POSTW - 3][i][e] = fmaf(dz, ve, q[NM + Q_POSTW - 3][i][e]);
+                            q[NM + Q_POSTB - 3][i][e] += dz;
+                        }
+                        const float dv = dz * w[i][e];
+                        H[i][e] = dv;
+                        s1 += dv;
+                        s2 = fmaf(dv, ve, s2);
+                    }
+            }
+            if (dy == nullptr) continue;
+            if (a.post != 0) {
+                Team<TPR>::sum2(s1, s2, red);
+                const float k1 = a.post == NORM_LAYER ? s1 / (float)a.C : 0.f, k2 = s2 / (float)a.C;
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) H[i][e] = ry * (H[i][e] - k1 - v[i][e] * k2);
+            }
+            r.store(dy + at, H);
+        }
+#pragma unroll
+        for (int k = 0; k < NM; ++k) {
+            if (g.out[k] == nullptr) continue;
+            flush(q[k], g.per_group == 1 ? g.out[k] + (long)group * a.C : g.slots + ((long)k * g.n_items + item) * a.C,
+                  !g.alone);
+        }
+    }
+    if constexpr (NV > 0) {
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (g.out[3 + k] != nullptr) flush(q[NM + k], g.sums + ((long)k * gridDim.x + blockIdx.x) * a.C, true);
+    }
+}
+
+// Adds items (group blockIdx.y) or blocks: 16 slices of them by 16 threads of
+// four channels each, then the slices.
+__global__ __launch_bounds__(256) void k_norm_grad_join(int C, int blocks, GradItems g) {
+    __shared__ f32x4 part[16][16];
+    const int k = blockIdx.z, lane = threadIdx.x & 15, slice = threadIdx.x >> 4, c = blockIdx.x * 64 + lane * 4;
+    const long group = blockIdx.y;
+    const bool vec = k >= 3;
+    if (g.out[k] == nullptr || (vec ? group > 0 : g.per_group == 1)) return;
+    const int n = vec ? blocks : g.per_group;
+    const float *src = vec ? g.sums + (long)(k - 3) * blocks * C : g.slots + ((long)k * g.n_items + group * n) * C;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (c < C)
+        for (int i = slice; i < n; i += 16) s += *reinterpret_cast<const f32x4 *>(src + (long)i * C + c);
+    part[slice][lane] = s;
+    __syncthreads();
+    if (slice > 0 || c >= C) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += part[i][lane];
+    *reinterpret_cast<f32x4 *>(g.out[k] + (vec ? 0 : group * C) + c) = s;
 }
 
 // Rows too long for that: read again for every pass over them.
@@ -329,7 +527,7 @@ struct GradRow : NormRow<T> {
 };
 
 template <typename T>
-__global__ __launch_bounds__(256) void k_norm_grad_rows(NormArgs a, const T *dh, const T *dn, T *dx, T *dy,
+__global__ __launch_bounds__(256) void k_norm_grad_rows_wide(NormArgs a, const T *dh, const T *dn, T *dx, T *dy,
                                                         RowStats *rows) {
     __shared__ float red[4];
     const long row = folded_block();
@@ -398,7 +596,6 @@ __global__ __launch_bounds__(256) void k_norm_grad_rows(NormArgs a, const T *dh,
 // out at every change of the modulation row: straight to the result where the
 // part holds all of its rows, else to one of two slots of the part (0: a
 // modulation row that an earlier part began, 1: one that this part begins).
-enum { Q_GATE, Q_SCALE, Q_SHIFT, Q_POSTW, Q_POSTB, Q_PREW, Q_PREB, N_Q };
 struct ColOut {
     float *out[N_Q];        // results, or NULL
     float *slots;           // [3][n_parts][2][C]
@@ -407,7 +604,7 @@ struct ColOut {
 };
 
 template <typename T>
-__global__ __launch_bounds__(64) void k_norm_grad_cols(NormArgs a, const T *dh, const T *dn, const RowStats *rows,
+__global__ __launch_bounds__(64) void k_norm_grad_cols_wide(NormArgs a, const T *dh, const T *dn, const RowStats *rows,
                                                        ColOut o) {
     const int c = (blockIdx.y * 64 + threadIdx.x) * 8, p = blockIdx.x;
     if (c >= a.C) return;
@@ -464,7 +661,7 @@ __global__ __launch_bounds__(64) void k_norm_grad_cols(NormArgs a, const T *dh, 
 
 // Joins the parts, in their order: block p > 0 the modulation row that is the
 // first to cross the start of part p, block 0 the vectors of all rows.
-__global__ __launch_bounds__(64) void k_norm_grad_join(int C, int rows, int rows_per_mod, ColOut o) {
+__global__ __launch_bounds__(64) void k_norm_grad_join_wide(int C, int rows, int rows_per_mod, ColOut o) {
     const int c = blockIdx.y * 64 + threadIdx.x, k = blockIdx.z;
     if (c >= C || o.out[k] == nullptr || (k < 3) != (blockIdx.x > 0)) return;
     float s = 0.f;
@@ -488,7 +685,7 @@ __global__ void k_zero(float *p, int n) {
 
 size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
 
-int norm_part(int rows) { return std::max(1, cdiv(rows, 1024)); }
+int wide_part(int rows) { return std::max(1, cdiv(rows, 1024)); }
 
 }  // namespace
 
@@ -498,20 +695,27 @@ hipError_t launch_zero(float *p, int n, hipStream_t st) {
 }
 
 // f(threads per row, chunks of 8 channels per thread) for a row of C channels;
-// (256, 0): too long for registers.  A wave for a row of up to 2048 where there
-// are rows for all units, else the block.
+// (256, 0): too long for registers.  The fewest lanes that hold a row in three
+// chunks (four from 1537 channels) where there are rows for all units: fewer
+// lanes idle and fewer steps in a sum; else the block.
 template <typename F>
 static hipError_t norm_shape(int rows, int C, F f) {
     using std::integral_constant;
     const int c = cdiv(C, 8);
     if (c <= 256 && rows >= 4 * N_CUS) {
+        constexpr integral_constant<int, 16> quarter{};
+        constexpr integral_constant<int, 32> half{};
         constexpr integral_constant<int, 64> wave{};
-        switch (cdiv(c, 64)) {
-            case 1: return f(wave, integral_constant<int, 1>{});
-            case 2: return f(wave, integral_constant<int, 2>{});
-            case 3: return f(wave, integral_constant<int, 3>{});
-            default: return f(wave, integral_constant<int, 4>{});
-        }
+        constexpr integral_constant<int, 1> one{};
+        constexpr integral_constant<int, 2> two{};
+        constexpr integral_constant<int, 3> three{};
+        if (c <= 16) return f(quarter, one);
+        if (c <= 32) return f(quarter, two);
+        if (c <= 48) return f(quarter, three);
+        if (c <= 64) return f(half, two);
+        if (c <= 96) return f(half, three);
+        if (c <= 128) return f(wave, two);
+        return c <= 192 ? f(wave, three) : f(wave, integral_constant<int, 4>{});
     }
     constexpr integral_constant<int, 256> block{};
     if (c <= 256) return f(block, integral_constant<int, 1>{});
@@ -536,40 +740,92 @@ hipError_t launch_norm_gate(const NormArgs &a, void *h, void *n, hipStream_t st)
     return a.bf16 ? go_norm_gate(a, (uint16_t *)h, (uint16_t *)n, st) : go_norm_gate(a, (float *)h, (float *)n, st);
 }
 
-size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod) {
-    if (rows <= 0) return 0;
-    const size_t parts = (size_t)cdiv(rows, norm_part(rows));
-    return up256((size_t)rows * sizeof(RowStats)) + up256((rows_per_mod > 0 ? 6 : 0) * parts * C * 4) +
-           up256(4 * parts * C * 4);
+constexpr int GRAD_BLOCKS = 1024;
+
+// The items of a gradient call by teams of TPR threads.
+template <int TPR>
+static GradItems grad_items(int rows, int rows_per_mod, int &blocks) {
+    constexpr int TEAMS = Team<TPR>::PER_BLOCK;
+    GradItems g{};
+    const int per = std::min(rows_per_mod, rows), n_mod = cdiv(rows, per);
+    g.alone = TEAMS > 1 && per < 2 * TEAMS;
+    // (an item's sums cost its share of LDS and of the join: at least four rows a team)
+    g.per_group = g.alone ? 1 : std::min(std::max(1, GRAD_BLOCKS / n_mod), cdiv(per, 4 * TEAMS));
+    g.part = cdiv(per, g.per_group);
+    g.per_group = cdiv(per, g.part);
+    g.n_items = n_mod * g.per_group;
+    blocks = std::min(g.alone ? cdiv(g.n_items, TEAMS) : g.n_items, GRAD_BLOCKS);
+    return g;
 }
 
-hipError_t launch_norm_gate_grad(const NormArgs &a, const void *dh, const void *dn, void *dx, void *dy,
-                                 const NormGrads &g, void *ws, hipStream_t st) {
-    StageScope _stage(st, "norm_gate_grad");
+// enough for every kernel choice: slots of at most GRAD_BLOCKS items (more only where each is a whole
+// modulation row and needs none) and sums of as many blocks; the long rows' statistics and parts
+size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod) {
+    if (rows <= 0) return 0;
+    const size_t items = std::min(rows, GRAD_BLOCKS);
+    const size_t wide = C > 8192 ? up256((size_t)rows * sizeof(RowStats)) : 0;
+    return wide + up256((rows_per_mod > 0 ? 6 : 0) * items * C * 4) + up256(4 * items * C * 4);
+}
+
+template <typename T, int TPR, int CH, int ACC>
+static hipError_t go_norm_grad(const NormArgs &a, const T *dh, const T *dn, T *dx, T *dy, const NormGrads &q, void *ws,
+                               hipStream_t st) {
+    int blocks = 0;
+    GradItems g = grad_items<TPR>(a.rows, a.rows_per_mod, blocks);
+    float *const out[N_Q] = {q.gate, q.scale, q.shift, q.post_w, q.post_b, q.pre_w, q.pre_b};
+    std::copy(out, out + N_Q, g.out);
+    g.slots = (float *)ws;
+    const size_t slots = (ACC & ACC_MODS) && g.per_group > 1 ? 3 * (size_t)g.n_items * a.C * 4 : 0;
+    g.sums = (float *)((char *)ws + up256(slots));
+    const size_t lds = TPR == 256 || ACC == 0 ? 0 : (size_t)256 * CH * 8 * 4;
+    launch_k(k_norm_grad<T, TPR, CH, ACC>, blocks, 256, lds, st, a, dh, dn, dx, dy, g);
+    if (slots > 0 || (ACC & ACC_VECS))
+        launch_k(k_norm_grad_join, dim3((unsigned)cdiv(a.C, 64), slots > 0 ? (unsigned)(g.n_items / g.per_group) : 1u, N_Q),
+                 256, 0, st, a.C, blocks, g);
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t go_norm_grad_wide(const NormArgs &a, const T *dh, const T *dn, T *dx, T *dy, const NormGrads &q,
+                                    void *ws, hipStream_t st) {
     RowStats *rows = (RowStats *)ws;
-    ColOut o{{g.gate, g.scale, g.shift, g.post_w, g.post_b, g.pre_w, g.pre_b}, nullptr, nullptr, 0, 0};
-    o.part = norm_part(a.rows);
+    ColOut o{{q.gate, q.scale, q.shift, q.post_w, q.post_b, q.pre_w, q.pre_b}, nullptr, nullptr, 0, 0};
+    o.part = wide_part(a.rows);
     o.n_parts = cdiv(a.rows, o.part);
-    const bool mods = g.gate || g.scale || g.shift, vecs = g.post_w || g.post_b || g.pre_w || g.pre_b;
+    const bool mods = q.gate || q.scale || q.shift, vecs = q.post_w || q.post_b || q.pre_w || q.pre_b;
     char *w = (char *)ws + up256((size_t)a.rows * sizeof(RowStats));
     o.slots = (float *)w;
     o.sums = (float *)(w + up256((mods ? 6 : 0) * (size_t)o.n_parts * a.C * 4));
-    const dim3 grid = folded_grid(a.rows, 256);
-    if (a.bf16)
-        launch_k(k_norm_grad_rows<uint16_t>, grid, 256, 0, st, a, (const uint16_t *)dh, (const uint16_t *)dn,
-                 (uint16_t *)dx, (uint16_t *)dy, rows);
-    else
-        launch_k(k_norm_grad_rows<float>, grid, 256, 0, st, a, (const float *)dh, (const float *)dn, (float *)dx,
-                 (float *)dy, rows);
+    launch_k(k_norm_grad_rows_wide<T>, folded_grid(a.rows, 256), 256, 0, st, a, dh, dn, dx, dy, rows);
     if (!mods && !vecs) return hipGetLastError();
-    const dim3 cgrid((unsigned)o.n_parts, (unsigned)cdiv(a.C, 512));
-    if (a.bf16)
-        launch_k(k_norm_grad_cols<uint16_t>, cgrid, 64, 0, st, a, (const uint16_t *)dh, (const uint16_t *)dn, rows, o);
-    else
-        launch_k(k_norm_grad_cols<float>, cgrid, 64, 0, st, a, (const float *)dh, (const float *)dn, rows, o);
-    launch_k(k_norm_grad_join, dim3((unsigned)o.n_parts, (unsigned)cdiv(a.C, 64), N_Q), 64, 0, st, a.C, a.rows,
+    launch_k(k_norm_grad_cols_wide<T>, dim3((unsigned)o.n_parts, (unsigned)cdiv(a.C, 512)), 64, 0, st, a, dh, dn, rows, o);
+    launch_k(k_norm_grad_join_wide, dim3((unsigned)o.n_parts, (unsigned)cdiv(a.C, 64), N_Q), 64, 0, st, a.C, a.rows,
              a.rows_per_mod, o);
     return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t type_norm_grad(const NormArgs &a, const T *dh, const T *dn, T *dx, T *dy, const NormGrads &q,
+                                 void *ws, hipStream_t st) {
+    const bool mods = q.gate || q.scale || q.shift, vecs = q.post_w || q.post_b || q.pre_w || q.pre_b;
+    return norm_shape(a.rows, a.C, [&](auto tpr, auto ch) -> hipError_t {
+        constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
+        if constexpr (CH == 0) {
+            return go_norm_grad_wide(a, dh, dn, dx, dy, q, ws, st);
+        } else {
+            if (vecs) return go_norm_grad<T, TPR, CH, ACC_MODS | ACC_VECS>(a, dh, dn, dx, dy, q, ws, st);
+            if (mods) return go_norm_grad<T, TPR, CH, ACC_MODS>(a, dh, dn, dx, dy, q, ws, st);
+            return go_norm_grad<T, TPR, CH, 0>(a, dh, dn, dx, dy, q, ws, st);
+        }
+    });
+}
+
+hipError_t launch_norm_gate_grad(const NormArgs &a, const void *dh, const void *dn, void *dx, void *dy,
+                                 const NormGrads &q, void *ws, hipStream_t st) {
+    StageScope _stage(st, "norm_gate_grad");
+    if (a.bf16)
+        return type_norm_grad(a, (const uint16_t *)dh, (const uint16_t *)dn, (uint16_t *)dx, (uint16_t *)dy, q, ws, st);
+    return type_norm_grad(a, (const float *)dh, (const float *)dn, (float *)dx, (float *)dy, q, ws, st);
 }
 
 }  // namespace oc

@@ -60,7 +60,7 @@ __device__ __forceinline__ float wave_max(float v) {
     return v;
 }
 
-// Sum and maximum over a wave in every lane: within rows of 16 lanes by DPP
+// Sum and maximum in every lane, within rows of 16 lanes by DPP
 // operands, across them by the swaps of rows and halves, no LDS.
 template <int CTRL>
 __device__ __forceinline__ uint32_t dpp_mov(uint32_t v) {
@@ -77,25 +77,33 @@ __device__ __forceinline__ void swap32(uint32_t v, uint32_t &a, uint32_t &b) {
     a = r[0];
     b = r[1];
 }
-template <typename Op>
-__device__ __forceinline__ uint32_t wave_all(uint32_t v, Op op) {
+// over aligned groups of LANES (16, 32 or 64) lanes
+template <int LANES, typename Op>
+__device__ __forceinline__ uint32_t lanes_all(uint32_t v, Op op) {
     v = op(v, dpp_mov<0xB1>(v));    // lane ^ 1
     v = op(v, dpp_mov<0x4E>(v));    // lane ^ 2
     v = op(v, dpp_mov<0x141>(v));   // mirrored in 8: the other four
     v = op(v, dpp_mov<0x140>(v));   // mirrored in 16: the other eight
     uint32_t a, b;
-    swap16(v, a, b);
-    v = op(a, b);
-    swap32(v, a, b);
-    return op(a, b);
+    if constexpr (LANES >= 32) {
+        swap16(v, a, b);
+        v = op(a, b);
+    }
+    if constexpr (LANES >= 64) {
+        swap32(v, a, b);
+        v = op(a, b);
+    }
+    return v;
 }
-__device__ __forceinline__ float wave_all_sum(float v) {
-    return __uint_as_float(wave_all(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+template <int LANES = 64>
+__device__ __forceinline__ float lanes_sum(float v) {
+    return __uint_as_float(lanes_all<LANES>(__float_as_uint(v), [](uint32_t a, uint32_t b) {
         return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
     }));
 }
-__device__ __forceinline__ uint32_t wave_all_max(uint32_t v) {
-    return wave_all(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+template <int LANES = 64>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+    return lanes_all<LANES>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
 // (value, index) arg-max merge: larger value wins, smaller index on ties.
