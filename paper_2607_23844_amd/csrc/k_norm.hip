@@ -202,186 +202,348 @@ __global__ __launch_bounds__(256) void k_norm_gate(NormArgs a, T *h, T *n) {
 }
 
 enum { Q_GATE, Q_SCALE, Q_SHIFT, Q_POSTW, Q_POSTB, Q_PREW, Q_PREB, N_Q };
-constexpr int ACC_MODS = 1, ACC_VECS = 2;   // sums that a gradient call keeps
-
-// Work of the gradients: item i is rows [start, end) of one modulation row,
-// group i / per_group, split into per_group items.
+// Work of the gradients: item i is rows of one modulation row, group
+// i / per_group, split into per_group items.
 struct GradItems {
     float *out[N_Q];        // results, or NULL
     float *slots;           // [3][n_items][C], per_group > 1
     float *sums;            // [4][blocks][C]
     int part, per_group, n_items;   // rows of an item
-    int alone;              // a team takes an item by itself (else the block's teams share it)
 };
 
-// The gradients of rows in registers: x, y, dh, dn are read and dx, dy written
-// once, which bounds it.  Sums over rows stay in registers over an item (the
-// modulation's) or all items of the block (the norms' vectors); the block's
-// teams are added in LDS, blocks by k_norm_grad_join, in the order of their
-// numbers.
-template <typename T, int TPR, int CH, int ACC>
+// A row of 8 elements per chunk, kept as it was read.
+template <typename T> struct Raw8 { uint4 v[sizeof(T) / 2]; };
+__device__ __forceinline__ void widen(const Raw8<uint16_t> &r, float (&v)[8]) {
+    const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void widen(const Raw8<float> &r, float (&v)[8]) {
+    const uint32_t w[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+}
+
+// The gradients of rows in registers.  What a row needs of the vectors of its
+// modulation row are three products,
+//   P = g w_post, Q = g b_post, R = (1 + s) w:   h = rs x + P v + Q, da w = R dn, dz w_post = P H,
+// and all sums over rows follow from four,
+//   A = sum dn u, B = sum dn, C = sum H v, D = sum H:
+//   ds = w A + b B, dt = B, dw = (1 + s) A, db = (1 + s) B,
+//   dg = w_post C + b_post D, dw_post = g C, db_post = g D,
+// which takes 28 operations an element instead of 63 (at 64 lanes a clock and
+// unit the vector pipes would bound it) and four sums in registers instead of
+// seven.  x, y, dh and dn of a team's next row are on their way while it works
+// on one.  Sums leave an item through LDS (the block's teams, in order); those
+// of the norms' vectors are added up per block, and k_norm_grad_join adds the
+// blocks, in order.
+// ALONE: modulation rows of few rows each; a team takes a whole one, with P, Q
+// and R in registers, and keeps the vectors' sums there.
+template <typename T, int TPR, int CH, bool SUMS, bool ALONE>
 __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, const T *dn, T *dx, T *dy, GradItems g) {
     typedef RegRow<T, TPR, CH> Row;
     typedef typename Row::Vals Vals;
-    constexpr int TEAMS = Team<TPR>::PER_BLOCK;
-    constexpr int NM = ACC & ACC_MODS ? 3 : 0, NV = ACC & ACC_VECS ? 4 : 0;
-    extern __shared__ __align__(16) float comb[];   // [team][TPR * CH * 8], TEAMS > 1
+    constexpr int TEAMS = Team<TPR>::PER_BLOCK, CP = TPR * CH * 8;
+    extern __shared__ __align__(16) float lds[];   // P, Q, R [2][CP / 2] each (not ALONE); [team][CP]
+    float *const comb = lds + (ALONE ? 0 : 3 * CP);
     __shared__ float red[8];
     const Row r(a.C);
-    const int team = Team<TPR>::id();
-    Vals q[NM + NV > 0 ? NM + NV : 1];
-#pragma unroll
-    for (int k = 0; k < NM + NV; ++k)
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) q[k][i][e] = 0.f;
-    // the block's sum of v to `to`
-    auto flush = [&](Vals &v, float *to, bool shared) {
-        if (TEAMS == 1 || !shared) {
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-                if (r.in(i)) store8(to + r.at(i), v[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < CH; ++i) store8(comb + team * (TPR * CH * 8) + r.at(i), v[i]);
-            __syncthreads();
-            for (int c = threadIdx.x * 4; c < a.C; c += 1024) {
-                f32x4 s = *reinterpret_cast<const f32x4 *>(comb + c);
-#pragma unroll
-                for (int t = 1; t < TEAMS; ++t) s += *reinterpret_cast<const f32x4 *>(comb + t * (TPR * CH * 8) + c);
-                *reinterpret_cast<f32x4 *>(to + c) = s;
-            }
-            __syncthreads();
-        }
+    const int team = Team<TPR>::id(), lane = Team<TPR>::lane();
+    Vals sum[SUMS ? 4 : 1], vec[SUMS && ALONE ? 4 : 1], own[ALONE ? 3 : 1];
+    auto clear = [&](Vals &v) {
 #pragma unroll
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
     };
-    const int first = g.alone ? (int)blockIdx.x * TEAMS + team : (int)blockIdx.x;
-    const int items = (int)gridDim.x * (g.alone ? TEAMS : 1);
+    if constexpr (SUMS) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            clear(sum[k]);
+            if constexpr (ALONE) clear(vec[k]);
+        }
+    }
+    // P, Q and R of eight channels
+    auto products = [&](long mod, int c, float (&P)[8], float (&Q)[8], float (&R)[8]) {
+        float gt[8], s[8];
+        load8_or((const T *)a.post_w, c, 1.f, P);
+        load8_or((const T *)a.post_b, c, 0.f, Q);
+        load8_or((const T *)a.pre_w, c, 1.f, R);
+        load8_or((const T *)a.gate, mod + c, 1.f, gt);
+        load8_or((const T *)a.scale, mod + c, 0.f, s);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            P[e] *= gt[e];
+            Q[e] *= gt[e];
+            R[e] *= 1.f + s[e];
+        }
+    };
+    // (the two halves of a chunk lie apart, so that lanes read consecutive 16 bytes)
+    auto cst = [&](int k, int i, float (&v)[8]) {
+        if constexpr (ALONE) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = own[k][i][e];
+        } else {
+            const float *at = lds + k * CP + (lane + i * TPR) * 4;
+            *reinterpret_cast<f32x4 *>(v) = *reinterpret_cast<const f32x4 *>(at);
+            *reinterpret_cast<f32x4 *>(v + 4) = *reinterpret_cast<const f32x4 *>(at + CP / 2);
+        }
+    };
+    Raw8<T> rx[CH], ry[CH], rn[CH], rh[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) rx[i] = ry[i] = rn[i] = rh[i] = Raw8<T>{};
+    auto fetch = [&](const T *p, long at, Raw8<T> (&raw)[CH]) {
+        if (p == nullptr) return;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+            if (r.in(i)) {
+#pragma unroll
+                for (int k = 0; k < (int)sizeof(T) / 2; ++k)
+                    raw[i].v[k] = reinterpret_cast<const uint4 *>(p + at + r.at(i))[k];
+            }
+    };
+    auto fetch_row = [&](long row) {
+        const long at = row * a.C;
+        fetch((const T *)a.y, at, ry);
+        fetch((const T *)a.x, at, rx);
+        fetch(dn, at, rn);
+        fetch(dh, at, rh);
+    };
+    const int first = ALONE ? (int)blockIdx.x * TEAMS + team : (int)blockIdx.x;
+    const int items = (int)gridDim.x * (ALONE ? TEAMS : 1);
+    constexpr int STEP = ALONE ? 1 : TEAMS;
+    const float rs = a.y != nullptr ? a.res_scale : 1.f, per_c = 1.f / (float)a.C;
     for (int item = first; item < g.n_items; item += items) {
         const int group = item / g.per_group;
         const long start = (long)group * a.rows_per_mod + (long)(item - group * g.per_group) * g.part;
         const long stop = min(min(start + g.part, (long)(group + 1) * a.rows_per_mod), (long)a.rows);
         const long mod = group * a.ld;
-        for (long row = start + (g.alone ? 0 : team); row < stop; row += g.alone ? 1 : TEAMS) {
-            const long at = row * a.C;
-            Vals u, v, t, H, w, b;
-            r.load((const T *)a.x + at, u, 0.f);
-            r.load(dn != nullptr ? dn + at : nullptr, t, 0.f);
-            float ry = 1.f;
-            if (a.y != nullptr) {
-                r.load((const T *)a.y + at, v, 0.f);
-                ry = r.normalise(a.post, a.post_eps, v, red);
-                Vals gt;
-                r.load((const T *)a.post_w, w, 1.f);
-                r.load((const T *)a.post_b, b, 0.f);
-                r.load(a.gate != nullptr ? (const T *)a.gate + mod : nullptr, gt, 1.f);
+        long row = start + (ALONE ? 0 : team);
+        if (row < stop) fetch_row(row);
+        if constexpr (ALONE) {
 #pragma unroll
-                for (int i = 0; i < CH; ++i)
+            for (int i = 0; i < CH; ++i)
+                if (r.in(i)) products(mod, r.at(i), own[0][i], own[1][i], own[2][i]);
+                else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        u[i][e] = fmaf(gt[i][e], fmaf(v[i][e], w[i][e], b[i][e]), a.res_scale * u[i][e]);
+                    for (int e = 0; e < 8; ++e) own[0][i][e] = own[1][i][e] = own[2][i][e] = 0.f;
+                }
+        } else {
+            __syncthreads();   // the last item's products may still be read
+            for (int c8 = threadIdx.x; c8 < CP / 8; c8 += 256) {
+                float v[3][8] = {};
+                if (c8 * 8 < a.C) products(mod, c8 * 8, v[0], v[1], v[2]);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    *reinterpret_cast<f32x4 *>(lds + k * CP + c8 * 4) = *reinterpret_cast<const f32x4 *>(v[k]);
+                    *reinterpret_cast<f32x4 *>(lds + k * CP + CP / 2 + c8 * 4) = *reinterpret_cast<const f32x4 *>(v[k] + 4);
+                }
             }
-            r.load(dh != nullptr ? dh + at : nullptr, H, 0.f);
-            const float rh = r.normalise(a.pre, a.pre_eps, u, red);
+            __syncthreads();
+        }
+        while (row < stop) {
+            const long at = row * a.C;
+            Vals u, v, t, H;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                widen(ry[i], v[i]);
+                widen(rx[i], u[i]);
+                widen(rn[i], t[i]);
+                widen(rh[i], H[i]);
+            }
+            row += STEP;
+            if (row < stop) fetch_row(row);
+            float r_y = 1.f;
+            if (a.y != nullptr) {
+                r_y = r.normalise(a.post, a.post_eps, v, red);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    float P[8], Q[8];
+                    cst(0, i, P);
+                    cst(1, i, Q);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[i][e] = fmaf(v[i][e], P[e], fmaf(u[i][e], rs, Q[e]));
+                }
+            }
+            const float r_h = r.normalise(a.pre, a.pre_eps, u, red);
             float s1 = 0.f, s2 = 0.f;
-            {
-                Vals s;
-                r.load((const T *)a.pre_w, w, 1.f);
-                r.load((const T *)a.pre_b, b, 0.f);
-                r.load(a.scale != nullptr ? (const T *)a.scale + mod : nullptr, s, 0.f);
 #pragma unroll
-                for (int i = 0; i < CH; ++i)
+            for (int i = 0; i < CH; ++i) {
+                float R[8];
+                cst(2, i, R);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float d = t[i][e], da = d * (1.f + s[i][e]), ue = u[i][e];
-                        if constexpr (NM > 0) {
-                            q[Q_SCALE][i][e] = fmaf(d, fmaf(ue, w[i][e], b[i][e]), q[Q_SCALE][i][e]);
-                            q[Q_SHIFT][i][e] += d;
-                        }
-                        if constexpr (NV > 0) {
-                            q[NM + Q_PREW - 3][i][e] = fmaf(da, ue, q[NM + Q_PREW - 3][i][e]);
-                            q[NM + Q_PREB - 3][i][e] += da;
-                        }
-                        const float dv = da * w[i][e];
-                        t[i][e] = dv;
-                        s1 += dv;
-                        s2 = fmaf(dv, ue, s2);
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (SUMS) {
+                        sum[0][i][e] = fmaf(t[i][e], u[i][e], sum[0][i][e]);
+                        sum[1][i][e] += t[i][e];
                     }
+                    t[i][e] *= R[e];
+                    s1 += t[i][e];
+                    s2 = fmaf(t[i][e], u[i][e], s2);
+                }
             }
             float m1 = 0.f, m2 = 0.f;
             if (a.pre != 0) {
                 Team<TPR>::sum2(s1, s2, red);
-                m1 = a.pre == NORM_LAYER ? s1 / (float)a.C : 0.f;
-                m2 = s2 / (float)a.C;
+                m1 = a.pre == NORM_LAYER ? s1 * per_c : 0.f;
+                m2 = s2 * per_c;
             }
-            const float rs = a.y != nullptr ? a.res_scale : 1.f;
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    // (past C: not the means' share)
-                    H[i][e] = r.in(i) ? fmaf(rh, t[i][e] - m1 - u[i][e] * m2, H[i][e]) : 0.f;
+                    H[i][e] = fmaf(r_h, fmaf(-u[i][e], m2, t[i][e] - m1), H[i][e]);
                     u[i][e] = rs * H[i][e];
                 }
             if (dx != nullptr) r.store(dx + at, u);
             if (a.y == nullptr) continue;
             s1 = s2 = 0.f;
-            {
-                Vals gt;
-                r.load((const T *)a.post_w, w, 1.f);
-                r.load((const T *)a.post_b, b, 0.f);
-                r.load(a.gate != nullptr ? (const T *)a.gate + mod : nullptr, gt, 1.f);
 #pragma unroll
-                for (int i = 0; i < CH; ++i)
+            for (int i = 0; i < CH; ++i) {
+                float P[8];
+                cst(0, i, P);   // (0 past C, where H is the mean's share only)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float ve = v[i][e], he = H[i][e], dz = he * gt[i][e];
-                        if constexpr (NM > 0)
-                            q[Q_GATE][i][e] = fmaf(he, fmaf(ve, w[i][e], b[i][e]), q[Q_GATE][i][e]);
-                        if constexpr (NV > 0) {
-                            q[NM + Q_POSTW - 3][i][e] = fmaf(dz, ve, q[NM + Q_POSTW - 3][i][e]);
-                            q[NM + Q_POSTB - 3][i][e] += dz;
-                        }
-                        const float dv = dz * w[i][e];
-                        H[i][e] = dv;
-                        s1 += dv;
-                        s2 = fmaf(dv, ve, s2);
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (SUMS) {
+                        sum[2][i][e] = fmaf(H[i][e], v[i][e], sum[2][i][e]);
+                        sum[3][i][e] += H[i][e];
                     }
+                    H[i][e] *= P[e];
+                    s1 += H[i][e];
+                    s2 = fmaf(H[i][e], v[i][e], s2);
+                }
             }
             if (dy == nullptr) continue;
             if (a.post != 0) {
                 Team<TPR>::sum2(s1, s2, red);
-                const float k1 = a.post == NORM_LAYER ? s1 / (float)a.C : 0.f, k2 = s2 / (float)a.C;
+                const float k1 = a.post == NORM_LAYER ? s1 * per_c : 0.f, k2 = s2 * per_c;
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) H[i][e] = ry * (H[i][e] - k1 - v[i][e] * k2);
+                    for (int e = 0; e < 8; ++e) H[i][e] = r_y * fmaf(-v[i][e], k2, H[i][e] - k1);
             }
             r.store(dy + at, H);
         }
+        if constexpr (SUMS) {
+            // the sums of N channels from c on, to the gradients that they make
+            auto emit = [&](int c, auto width, const float *sa, const float *sb, const float *sc, const float *sd) {
+                constexpr int N = decltype(width)::value;
+                auto vector = [&](const void *p, long at, float other, float (&v)[N]) {
 #pragma unroll
-        for (int k = 0; k < NM; ++k) {
-            if (g.out[k] == nullptr) continue;
-            flush(q[k], g.per_group == 1 ? g.out[k] + (long)group * a.C : g.slots + ((long)k * g.n_items + item) * a.C,
-                  !g.alone);
+                    for (int e = 0; e < N; ++e) v[e] = p != nullptr ? Elem<T>::ld((const T *)p + at + e) : other;
+                };
+                float w[N], b[N], m[N], o[3][N];
+                vector(a.post_w, c, 1.f, w);
+                vector(a.post_b, c, 0.f, b);
+#pragma unroll
+                for (int e = 0; e < N; ++e) o[0][e] = fmaf(w[e], sc[e], b[e] * sd[e]);
+                vector(a.pre_w, c, 1.f, w);
+                vector(a.pre_b, c, 0.f, b);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    o[1][e] = fmaf(w[e], sa[e], b[e] * sb[e]);
+                    o[2][e] = sb[e];
+                }
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                    if (g.out[k] == nullptr) continue;
+                    float *const to =
+                        (g.per_group == 1 ? g.out[k] + (long)group * a.C : g.slots + ((long)k * g.n_items + item) * a.C) + c;
+#pragma unroll
+                    for (int e = 0; e < N; e += 4) *reinterpret_cast<f32x4 *>(to + e) = *reinterpret_cast<f32x4 *>(&o[k][e]);
+                }
+                // the norms' vectors: w_post, b_post, w, b
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (g.out[3 + k] == nullptr) continue;
+                    if (k == 0) vector(a.gate, mod + c, 1.f, m);
+                    if (k == 1) vector(a.gate, mod + c, 1.f, m);
+                    if (k >= 2) {
+                        vector(a.scale, mod + c, 0.f, m);
+#pragma unroll
+                        for (int e = 0; e < N; ++e) m[e] += 1.f;
+                    }
+                    const float *const of = k == 0 ? sc : k == 1 ? sd : k == 2 ? sa : sb;
+                    if constexpr (ALONE) {
+#pragma unroll
+                        for (int i = 0; i < CH; ++i)
+                            if (r.at(i) == c) {
+#pragma unroll
+                                for (int e = 0; e < N; ++e) vec[k][i][e] = fmaf(m[e], of[e], vec[k][i][e]);
+                            }
+                    } else {
+                        float *const to = g.sums + ((long)k * gridDim.x + blockIdx.x) * a.C + c;
+#pragma unroll
+                        for (int e = 0; e < N; e += 4) {
+                            f32x4 v = {m[e] * of[e], m[e + 1] * of[e + 1], m[e + 2] * of[e + 2], m[e + 3] * of[e + 3]};
+                            if (item != first) v += *reinterpret_cast<const f32x4 *>(to + e);
+                            *reinterpret_cast<f32x4 *>(to + e) = v;
+                        }
+                    }
+                }
+            };
+            if constexpr (ALONE || TEAMS == 1) {
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+                    if (r.in(i)) emit(r.at(i), std::integral_constant<int, 8>{}, sum[0][i], sum[1][i], sum[2][i], sum[3][i]);
+            } else {
+                // the teams' sums: this thread's channels, four at a time (CP is a multiple of 128)
+                constexpr int MINE = (CP + 1023) / 1024;
+                f32x4 tot[4][MINE];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) store8(comb + team * CP + r.at(i), sum[k][i]);
+                    __syncthreads();
+#pragma unroll
+                    for (int j = 0; j < MINE; ++j) {
+                        const int c = threadIdx.x * 4 + j * 1024;
+                        if (c >= CP) continue;
+                        f32x4 v = *reinterpret_cast<const f32x4 *>(comb + c);
+#pragma unroll
+                        for (int o = 1; o < TEAMS; ++o) v += *reinterpret_cast<const f32x4 *>(comb + o * CP + c);
+                        tot[k][j] = v;
+                    }
+                    __syncthreads();
+                }
+#pragma unroll
+                for (int j = 0; j < MINE; ++j) {
+                    const int c = threadIdx.x * 4 + j * 1024;
+                    if (c < a.C)
+                        emit(c, std::integral_constant<int, 4>{}, (const float *)&tot[0][j], (const float *)&tot[1][j],
+                             (const float *)&tot[2][j], (const float *)&tot[3][j]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) clear(sum[k]);
         }
     }
-    if constexpr (NV > 0) {
-        __syncthreads();
+    if constexpr (SUMS && ALONE) {
+        // the teams' sums of the norms' vectors
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (g.out[3 + k] != nullptr) flush(q[NM + k], g.sums + ((long)k * gridDim.x + blockIdx.x) * a.C, true);
+        for (int k = 0; k < 4; ++k) {
+            if (g.out[3 + k] == nullptr) continue;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < CH; ++i) store8(comb + team * CP + r.at(i), vec[k][i]);
+            __syncthreads();
+            for (int c = threadIdx.x * 4; c < a.C; c += 1024) {
+                f32x4 v = *reinterpret_cast<const f32x4 *>(comb + c);
+#pragma unroll
+                for (int o = 1; o < TEAMS; ++o) v += *reinterpret_cast<const f32x4 *>(comb + o * CP + c);
+                *reinterpret_cast<f32x4 *>(g.sums + ((long)k * gridDim.x + blockIdx.x) * a.C + c) = v;
+            }
+        }
     }
 }
 
-// Adds items (group blockIdx.y) or blocks: 16 slices of them by 16 threads of
+// Adds items (group blockIdx.y) or blocks: 64 slices of them by 16 threads of
 // four channels each, then the slices.
-__global__ __launch_bounds__(256) void k_norm_grad_join(int C, int blocks, GradItems g) {
-    __shared__ f32x4 part[16][16];
+__global__ __launch_bounds__(1024) void k_norm_grad_join(int C, int blocks, GradItems g) {
+    __shared__ f32x4 part[64][16];
     const int k = blockIdx.z, lane = threadIdx.x & 15, slice = threadIdx.x >> 4, c = blockIdx.x * 64 + lane * 4;
     const long group = blockIdx.y;
     const bool vec = k >= 3;
@@ -390,12 +552,18 @@ __global__ __launch_bounds__(256) void k_norm_grad_join(int C, int blocks, GradI
     const float *src = vec ? g.sums + (long)(k - 3) * blocks * C : g.slots + ((long)k * g.n_items + group * n) * C;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (c < C)
-        for (int i = slice; i < n; i += 16) s += *reinterpret_cast<const f32x4 *>(src + (long)i * C + c);
+        for (int i = slice; i < n; i += 64) s += *reinterpret_cast<const f32x4 *>(src + (long)i * C + c);
     part[slice][lane] = s;
+    __syncthreads();
+    if (slice < 8) {
+#pragma unroll
+        for (int i = 8; i < 64; i += 8) s += part[slice + i][lane];
+        part[slice][lane] = s;
+    }
     __syncthreads();
     if (slice > 0 || c >= C) return;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) s += part[i][lane];
+    for (int i = 1; i < 8; ++i) s += part[i][lane];
     *reinterpret_cast<f32x4 *>(g.out[k] + (vec ? 0 : group * C) + c) = s;
 }
 
@@ -740,21 +908,26 @@ hipError_t launch_norm_gate(const NormArgs &a, void *h, void *n, hipStream_t st)
     return a.bf16 ? go_norm_gate(a, (uint16_t *)h, (uint16_t *)n, st) : go_norm_gate(a, (float *)h, (float *)n, st);
 }
 
-constexpr int GRAD_BLOCKS = 1024;
+// (512 blocks: 230400 x 320 210 us and 30000 x 1536 127 against 224 and 136 with 1024, whose partial sums
+// weigh more; 256: 205 and 124, but 71 against 56 at 230400 x 64)
+constexpr int GRAD_BLOCKS = 512;
 
-// The items of a gradient call by teams of TPR threads.
-template <int TPR>
-static GradItems grad_items(int rows, int rows_per_mod, int &blocks) {
-    constexpr int TEAMS = Team<TPR>::PER_BLOCK;
+// Whether a team takes the rows of a modulation row alone, and the items of a
+// gradient call by blocks of `teams` teams.
+static bool grad_alone(int rows, int rows_per_mod, int teams) {
+    return teams > 1 && std::min(rows_per_mod, rows) < std::max(2 * teams, 16);
+}
+static GradItems grad_items(int rows, int rows_per_mod, int teams, int &blocks) {
     GradItems g{};
     const int per = std::min(rows_per_mod, rows), n_mod = cdiv(rows, per);
-    g.alone = TEAMS > 1 && per < 2 * TEAMS;
-    // (an item's sums cost its share of LDS and of the join: at least four rows a team)
-    g.per_group = g.alone ? 1 : std::min(std::max(1, GRAD_BLOCKS / n_mod), cdiv(per, 4 * TEAMS));
+    const bool alone = grad_alone(rows, rows_per_mod, teams);
+    // (an item's sums cost its share of LDS and of the join: four rows a team where that leaves no unit idle)
+    const int least = std::min(std::max(rows / (N_CUS * teams), 1), 4) * teams;
+    g.per_group = alone ? 1 : std::min(std::max(1, GRAD_BLOCKS / n_mod), cdiv(per, least));
     g.part = cdiv(per, g.per_group);
     g.per_group = cdiv(per, g.part);
     g.n_items = n_mod * g.per_group;
-    blocks = std::min(g.alone ? cdiv(g.n_items, TEAMS) : g.n_items, GRAD_BLOCKS);
+    blocks = std::min(alone ? cdiv(g.n_items, teams) : g.n_items, GRAD_BLOCKS);
     return g;
 }
 
@@ -767,21 +940,25 @@ size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod) {
     return wide + up256((rows_per_mod > 0 ? 6 : 0) * items * C * 4) + up256(4 * items * C * 4);
 }
 
-template <typename T, int TPR, int CH, int ACC>
+template <typename T, int TPR, int CH, bool SUMS, bool ALONE>
 static hipError_t go_norm_grad(const NormArgs &a, const T *dh, const T *dn, T *dx, T *dy, const NormGrads &q, void *ws,
                                hipStream_t st) {
+    constexpr int TEAMS = Team<TPR>::PER_BLOCK, CP = TPR * CH * 8;
     int blocks = 0;
-    GradItems g = grad_items<TPR>(a.rows, a.rows_per_mod, blocks);
+    GradItems g = grad_items(a.rows, a.rows_per_mod, TEAMS, blocks);
     float *const out[N_Q] = {q.gate, q.scale, q.shift, q.post_w, q.post_b, q.pre_w, q.pre_b};
     std::copy(out, out + N_Q, g.out);
+    const bool mods = q.gate || q.scale || q.shift, vecs = q.post_w || q.post_b || q.pre_w || q.pre_b;
     g.slots = (float *)ws;
-    const size_t slots = (ACC & ACC_MODS) && g.per_group > 1 ? 3 * (size_t)g.n_items * a.C * 4 : 0;
+    const size_t slots = mods && g.per_group > 1 ? 3 * (size_t)g.n_items * a.C * 4 : 0;
     g.sums = (float *)((char *)ws + up256(slots));
-    const size_t lds = TPR == 256 || ACC == 0 ? 0 : (size_t)256 * CH * 8 * 4;
-    launch_k(k_norm_grad<T, TPR, CH, ACC>, blocks, 256, lds, st, a, dh, dn, dx, dy, g);
-    if (slots > 0 || (ACC & ACC_VECS))
+    const size_t lds = ((ALONE ? 0 : 3) + (SUMS && (ALONE || TEAMS > 1) ? TEAMS : 0)) * (size_t)CP * 4;
+    const hipError_t e = raise_lds_limit((const void *)k_norm_grad<T, TPR, CH, SUMS, ALONE>, lds);
+    if (e != hipSuccess) return e;
+    launch_k(k_norm_grad<T, TPR, CH, SUMS, ALONE>, blocks, 256, lds, st, a, dh, dn, dx, dy, g);
+    if (slots > 0 || vecs)
         launch_k(k_norm_grad_join, dim3((unsigned)cdiv(a.C, 64), slots > 0 ? (unsigned)(g.n_items / g.per_group) : 1u, N_Q),
-                 256, 0, st, a.C, blocks, g);
+                 1024, 0, st, a.C, blocks, g);
     return hipGetLastError();
 }
 
@@ -804,18 +981,47 @@ static hipError_t go_norm_grad_wide(const NormArgs &a, const T *dh, const T *dn,
     return hipGetLastError();
 }
 
+// As norm_shape, in two chunks where it can (a row's values, gradients and sums
+// take over 12 registers a channel).
+template <typename F>
+static hipError_t grad_shape(int rows, int C, F f) {
+    using std::integral_constant;
+    const int c = cdiv(C, 8);
+    constexpr integral_constant<int, 1> one{};
+    constexpr integral_constant<int, 2> two{};
+    if (c <= 256 && rows >= 4 * N_CUS) {
+        constexpr integral_constant<int, 16> quarter{};
+        constexpr integral_constant<int, 32> half{};
+        constexpr integral_constant<int, 64> wave{};
+        if (c <= 16) return f(quarter, one);
+        if (c <= 32) return f(quarter, two);
+        if (c <= 48) return f(quarter, integral_constant<int, 3>{});
+        if (c <= 64) return f(half, two);
+        if (c <= 128) return f(wave, two);
+        if (c <= 192) return f(wave, integral_constant<int, 3>{});
+    }
+    constexpr integral_constant<int, 256> block{};
+    if (c <= 256) return f(block, one);
+    if (c <= 512) return f(block, two);
+    return c <= 1024 ? f(block, integral_constant<int, 4>{}) : f(block, integral_constant<int, 0>{});
+}
+
 template <typename T>
 static hipError_t type_norm_grad(const NormArgs &a, const T *dh, const T *dn, T *dx, T *dy, const NormGrads &q,
                                  void *ws, hipStream_t st) {
     const bool mods = q.gate || q.scale || q.shift, vecs = q.post_w || q.post_b || q.pre_w || q.pre_b;
-    return norm_shape(a.rows, a.C, [&](auto tpr, auto ch) -> hipError_t {
+    return grad_shape(a.rows, a.C, [&](auto tpr, auto ch) -> hipError_t {
         constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
         if constexpr (CH == 0) {
             return go_norm_grad_wide(a, dh, dn, dx, dy, q, ws, st);
         } else {
-            if (vecs) return go_norm_grad<T, TPR, CH, ACC_MODS | ACC_VECS>(a, dh, dn, dx, dy, q, ws, st);
-            if (mods) return go_norm_grad<T, TPR, CH, ACC_MODS>(a, dh, dn, dx, dy, q, ws, st);
-            return go_norm_grad<T, TPR, CH, 0>(a, dh, dn, dx, dy, q, ws, st);
+            if constexpr (TPR < 256) {
+                if (grad_alone(a.rows, a.rows_per_mod, Team<TPR>::PER_BLOCK))
+                    return mods || vecs ? go_norm_grad<T, TPR, CH, true, true>(a, dh, dn, dx, dy, q, ws, st)
+                                        : go_norm_grad<T, TPR, CH, false, true>(a, dh, dn, dx, dy, q, ws, st);
+            }
+            return mods || vecs ? go_norm_grad<T, TPR, CH, true, false>(a, dh, dn, dx, dy, q, ws, st)
+                                : go_norm_grad<T, TPR, CH, false, false>(a, dh, dn, dx, dy, q, ws, st);
         }
     });
 }
