@@ -7,7 +7,6 @@ need not be the current one; the work goes on that GPU's current stream.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 from dataclasses import dataclass
 from typing import Dict, Optional, Sequence, Tuple
@@ -15,7 +14,7 @@ from typing import Dict, Optional, Sequence, Tuple
 import torch
 
 from . import _lib as L
-from .api import Rope, Shape, _ptr
+from .api import Rope, Shape
 
 
 @dataclass
@@ -37,20 +36,30 @@ class Mod:
     rows_per_mod: Optional[int] = None
 
 
-_SAME = contextlib.nullcontext()
-
-
-def _on(t: torch.Tensor):
-    """The tensor's GPU as the current one for the call's launches."""
-    return _SAME if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
-
-
-def _stream_of(t: torch.Tensor) -> int:
-    return torch.cuda.current_stream(t.device).cuda_stream
-
-
 def _bad(status: int, message: str):
     return L.OmniCacheError(status, message)
+
+
+def _call(name: str, dev: torch.device, *args) -> None:
+    """The C call with the stream last: the tensors' GPU as the current one for
+    its launches, and that GPU's current stream."""
+    fn, idx = getattr(L.lib(), name), dev.index
+    if torch._C._cuda_getDevice() == idx:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(idx))
+    else:
+        with torch.cuda.device(idx):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(idx))
+    if status:
+        L.check(status)
+
+
+def _struct(v):
+    """C.byref of the C struct of a Shape or Rope (immutable: made once)."""
+    ref = v.__dict__.get("_ref")
+    if ref is None:
+        ref = C.byref(v.c())
+        object.__setattr__(v, "_ref", ref)
+    return ref
 
 
 def _gpu(t, name: str) -> torch.Tensor:
@@ -63,24 +72,27 @@ def _like(t: Optional[torch.Tensor], shape, dtype, dev, name: str) -> Optional[i
     """The address of a contiguous tensor of this shape, type and GPU (None: NULL)."""
     if t is None:
         return None
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == dev and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
     if _gpu(t, name).dtype != dtype:
         raise _bad(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected {dtype}")
     if t.device != dev:
         raise _bad(L.OC_ERR_INVALID_ARG, f"{name} is on {t.device}, expected {dev}")
     if t.shape != shape:
         raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if not t.is_contiguous():
-        raise _bad(L.OC_ERR_INVALID_ARG, f"{name} must be contiguous")
-    return t.data_ptr()
+    raise _bad(L.OC_ERR_INVALID_ARG, f"{name} must be contiguous")
 
 
 def _norm(n: Optional[Norm], shape: Shape, dev, name: str) -> Optional[L.oc_norm]:
     if n is None:
         return None
-    if n.kind not in L.NORMS:
+    kind = L.NORMS.get(n.kind)
+    if kind is None:
         raise _bad(L.OC_ERR_INVALID_ARG, f"{name}: unknown norm {n.kind!r}")
+    if n.w is None and n.b is None:
+        return L.oc_norm(kind, n.eps)
     c, dt = (shape.C,), shape.torch_dtype
-    return L.oc_norm(L.NORMS[n.kind], n.eps, _like(n.w, c, dt, dev, name + ".w"), _like(n.b, c, dt, dev, name + ".b"))
+    return L.oc_norm(kind, n.eps, _like(n.w, c, dt, dev, name + ".w"), _like(n.b, c, dt, dev, name + ".b"))
 
 
 def _mod(m: Optional[Mod], rows: int, shape: Shape, dev) -> Optional[L.oc_mod]:
@@ -89,27 +101,26 @@ def _mod(m: Optional[Mod], rows: int, shape: Shape, dev) -> Optional[L.oc_mod]:
     per = max(rows, 1) if m.rows_per_mod is None else m.rows_per_mod
     if per < 1:
         raise _bad(L.OC_ERR_INVALID_ARG, f"rows_per_mod={per} must be >= 1")
-    n_mod, ld, at = -(-rows // per), None, []
+    n_mod, ld, at, dt, Ch = -(-rows // per), None, [], shape.torch_dtype, shape.C
     for name, t in (("gate", m.gate), ("scale", m.scale), ("shift", m.shift)):
         if t is None:
             at.append(None)
             continue
-        if _gpu(t, name).dtype != shape.torch_dtype:
-            raise _bad(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected {shape.torch_dtype}")
+        if _gpu(t, name).dtype != dt:
+            raise _bad(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected {dt}")
         if t.device != dev:
             raise _bad(L.OC_ERR_INVALID_ARG, f"{name} is on {t.device}, expected {dev}")
-        if t.dim() == 1:
-            t = t[None]
-        if t.shape != (n_mod, shape.C):
-            raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(t.shape)}, expected {(n_mod, shape.C)}")
-        if t.stride(1) != 1 and shape.C > 1:
+        size, step = t.shape, t.stride()
+        if size != (n_mod, Ch) and not (n_mod == 1 and size == (Ch,)):
+            raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(size)}, expected {(n_mod, Ch)}")
+        if step[-1] != 1:
             raise _bad(L.OC_ERR_INVALID_ARG, f"the channels of {name} must be contiguous")
-        row = t.stride(0) if n_mod > 1 else shape.C
+        row = step[0] if n_mod > 1 else Ch
         if ld is not None and row != ld:
             raise _bad(L.OC_ERR_INVALID_ARG, "gate, scale and shift must have the same row stride")
         ld = row
         at.append(t.data_ptr())
-    return L.oc_mod(*at, shape.C if ld is None else ld, per, 0)
+    return L.oc_mod(*at, Ch if ld is None else ld, per, 0)
 
 
 def _rows_of(x: torch.Tensor, shape: Shape) -> int:
@@ -139,18 +150,18 @@ def norm_gate(x: torch.Tensor, shape: Shape, y: Optional[torch.Tensor] = None, p
     n = torch.empty_like(x) if n is None else n
     hp = None if h is False else _like(h, full, dt, dev, "h")
     np_ = None if n is False else _like(n, full, dt, dev, "n")
-    sh, po, pr, mo = shape.c(), _norm(post, shape, dev, "post"), _norm(pre, shape, dev, "pre"), _mod(mod, rows, shape, dev)
+    po, pr, mo = _norm(post, shape, dev, "post"), _norm(pre, shape, dev, "pre"), _mod(mod, rows, shape, dev)
     if rows == 0:      # (empty tensors have no address)
         hp = np_ = xp = yp = None
-    with _on(x):
-        L.check(L.lib().oc_norm_gate(C.byref(sh), rows, xp, yp, _ref(po), _ref(pr), _ref(mo), res_scale, hp, np_,
-                                     _stream_of(x)))
+    _call("oc_norm_gate", dev, _struct(shape), rows, xp, yp, _ref(po), _ref(pr), _ref(mo), res_scale, hp, np_)
     return (x if y is None else None if h is False else h), (None if n is False else n)
 
 
+GRADS = ("dx", "dy", "gate", "scale", "shift", "post_w", "post_b", "pre_w", "pre_b")
+
+
 def norm_gate_grad_workspace_bytes(shape: Shape, rows: int, rows_per_mod: int = 0) -> int:
-    sh = shape.c()
-    return int(L.lib().oc_norm_gate_grad_workspace_bytes(C.byref(sh), rows, rows_per_mod))
+    return L.lib().oc_norm_gate_grad_workspace_bytes(_struct(shape), rows, rows_per_mod)
 
 
 def norm_gate_grad(x: torch.Tensor, shape: Shape, dn: Optional[torch.Tensor] = None,
@@ -166,56 +177,60 @@ def norm_gate_grad(x: torch.Tensor, shape: Shape, dn: Optional[torch.Tensor] = N
     dev, dt, full = x.device, shape.torch_dtype, x.shape
     xp, yp = _like(x, full, dt, dev, "x"), _like(y, full, dt, dev, "y")
     dnp, dhp = _like(dn, full, dt, dev, "dn"), _like(dh, full, dt, dev, "dh")
-    sh, po, pr, mo = shape.c(), _norm(post, shape, dev, "post"), _norm(pre, shape, dev, "pre"), _mod(mod, rows, shape, dev)
-    per = mo.rows_per_mod if mo is not None else 0
-    n_mod = -(-rows // per) if per else 0
-    has = {"dx": True, "dy": y is not None}
-    has.update({k: getattr(mo, k) is not None if mo is not None else False for k in ("gate", "scale", "shift")})
-    for k, s in (("post", po), ("pre", pr)):
-        has.update({k + "_w": s is not None and s.w is not None, k + "_b": s is not None and s.b is not None})
-    if want is not None and not set(want) <= set(has):
-        raise _bad(L.OC_ERR_INVALID_ARG, f"unknown gradients {sorted(set(want) - set(has))}")
-    out = {}
-    for k, there in has.items():
-        if not there or (want is not None and k not in want):
-            out[k] = None
-        elif k in ("dx", "dy"):
-            out[k] = torch.empty_like(x)
-        else:
-            out[k] = torch.empty((n_mod, shape.C) if k in ("gate", "scale", "shift") else (shape.C,),
+    po, pr, mo = _norm(post, shape, dev, "post"), _norm(pre, shape, dev, "pre"), _mod(mod, rows, shape, dev)
+    per, n_mod = 0, 0
+    has = [k for k, t in (("gate", mod and mod.gate), ("scale", mod and mod.scale), ("shift", mod and mod.shift),
+                          ("post_w", post and post.w), ("post_b", post and post.b), ("pre_w", pre and pre.w),
+                          ("pre_b", pre and pre.b)) if t is not None]
+    if mo is not None:
+        per = mo.rows_per_mod
+        n_mod = -(-rows // per)
+    out = dict.fromkeys(GRADS)
+    if want is not None:
+        if not set(want) <= set(GRADS):
+            raise _bad(L.OC_ERR_INVALID_ARG, f"unknown gradients {sorted(set(want) - set(GRADS))}")
+        has = [k for k in has if k in want]
+    at = dict(out)
+    for k in has:
+        t = out[k] = torch.empty((n_mod, shape.C) if k in ("gate", "scale", "shift") else (shape.C,),
                                  dtype=torch.float32, device=dev)
+        at[k] = t.data_ptr()
+    for k, there in (("dx", True), ("dy", y is not None)):
+        if there and (want is None or k in want):
+            out[k] = torch.empty_like(x)
+            at[k] = out[k].data_ptr()
     if ws is None:
         ws = torch.empty(max(norm_gate_grad_workspace_bytes(shape, rows, per), 256), dtype=torch.uint8, device=dev)
     elif _gpu(ws, "ws").device != dev or not ws.is_contiguous():
         raise _bad(L.OC_ERR_INVALID_ARG, f"ws must be contiguous and on {dev}")
-    g = L.oc_norm_grads(*(_ptr(out[k]) for k in ("gate", "scale", "shift", "post_w", "post_b", "pre_w", "pre_b")))
-    with _on(x):
-        L.check(L.lib().oc_norm_gate_grad(C.byref(sh), rows, xp, yp, _ref(po), _ref(pr), _ref(mo), res_scale, dhp, dnp,
-                                          _ptr(out["dx"]), _ptr(out["dy"]), C.byref(g), ws.data_ptr(),
-                                          ws.numel() * ws.element_size(), _stream_of(x)))
+    g = L.oc_norm_grads(*(at[k] for k in GRADS[2:]))
+    _call("oc_norm_gate_grad", dev, _struct(shape), rows, xp, yp, _ref(po), _ref(pr), _ref(mo), res_scale, dhp, dnp,
+          at["dx"], at["dy"], C.byref(g), ws.data_ptr(), ws.nbytes)
     return out
 
 
-def _heads_of(t: Optional[torch.Tensor], rows: Optional[int], heads: Optional[int], shape: Shape, dev, name: str):
+def _heads_of(t: Optional[torch.Tensor], rows: int, heads: Optional[int], shape: Shape, dev, name: str):
     """(address, row stride, heads) of a [rows, heads, head_dim] tensor whose
     rows hold their heads contiguously."""
     if t is None:
         return None, 0, 0
-    if _gpu(t, name).dtype != shape.torch_dtype:
-        raise _bad(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected {shape.torch_dtype}")
-    if dev is not None and t.device != dev:
+    dt, dh = shape.torch_dtype, shape.head_dim
+    if _gpu(t, name).dtype != dt:
+        raise _bad(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected {dt}")
+    if t.device != dev:
         raise _bad(L.OC_ERR_INVALID_ARG, f"{name} is on {t.device}, expected {dev}")
-    if t.dim() != 3 or t.shape[2] != shape.head_dim or (rows is not None and t.shape[0] != rows) or \
-            (heads is not None and t.shape[1] != heads):
-        raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(t.shape)}, expected "
-                                   f"{('rows' if rows is None else rows, 'heads' if heads is None else heads, shape.head_dim)}")
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != shape.head_dim):
+    size = t.shape
+    if len(size) != 3 or size[2] != dh or size[0] != rows or (heads is not None and size[1] != heads):
+        raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(size)}, expected "
+                                   f"{(rows, 'heads' if heads is None else heads, dh)}")
+    step = t.stride()
+    if step[2] != 1 or (size[1] > 1 and step[1] != dh):
         raise _bad(L.OC_ERR_INVALID_ARG, f"the heads of a row of {name} must be contiguous")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2], t.shape[1]
+    return t.data_ptr(), step[0] if rows > 1 else size[1] * dh, size[1]
 
 
 def _ids(t: Optional[torch.Tensor], shape, dev, name: str) -> Optional[int]:
-    return _like(t, torch.Size(shape), torch.int32, dev, name)
+    return _like(t, shape, torch.int32, dev, name)
 
 
 def rope_qk(q: Optional[torch.Tensor], k: Optional[torch.Tensor], rope: Rope, shape: Shape,
@@ -235,17 +250,19 @@ def rope_qk(q: Optional[torch.Tensor], k: Optional[torch.Tensor], rope: Rope, sh
     kp, ldk, kh = _heads_of(k, rows, None, shape, dev, "k")
     if q_out is None and q is not None:
         q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        qop, ldqo = q_out.data_ptr(), shape.heads * shape.head_dim
+    else:
+        qop, ldqo, _ = _heads_of(q_out, rows, shape.heads, shape, dev, "q_out")
     if k_out is None and k is not None:
         k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
-    qop, ldqo, _ = _heads_of(q_out, rows, shape.heads, shape, dev, "q_out")
-    kop, ldko, _ = _heads_of(k_out, rows, kh, shape, dev, "k_out")
+        kop, ldko = k_out.data_ptr(), kh * shape.head_dim
+    else:
+        kop, ldko, _ = _heads_of(k_out, rows, kh, shape, dev, "k_out")
     ip, pp = _ids(kept_idx, (rows,), dev, "kept_idx"), _ids(pos, (rows, 3), dev, "pos")
     if rows == 0:      # (empty tensors have no address)
         qp = kp = qop = kop = None
-    sh, ro = shape.c(), rope.c()
-    with _on(first):
-        L.check(L.lib().oc_rope_qk(C.byref(sh), C.byref(ro), rows, ip, pp, qp, ldq, kp, ldk, kh, qop, ldqo, kop, ldko,
-                                   1 if inverse else 0, _stream_of(first)))
+    _call("oc_rope_qk", dev, _struct(shape), _struct(rope), rows, ip, pp, qp, ldq, kp, ldk, kh, qop, ldqo, kop, ldko,
+          1 if inverse else 0)
     return q_out, k_out
 
 
@@ -258,9 +275,10 @@ def _matrix(t, name: str):
         raise _bad(L.OC_ERR_DTYPE, f"{name} has dtype {t.dtype}, expected bfloat16 or float32")
     if t.dim() != 2:
         raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(t.shape)}, expected two dimensions")
-    if t.stride(1) != 1 and t.shape[1] > 1:
+    size, step = t.shape, t.stride()
+    if step[1] != 1 and size[1] > 1:
         raise _bad(L.OC_ERR_INVALID_ARG, f"the rows of {name} must be contiguous")
-    return t.data_ptr() or None, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.data_ptr() or None, step[0] if size[0] > 1 else size[1]
 
 
 def quant_rows(x: torch.Tensor, row_idx: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
@@ -276,8 +294,7 @@ def quant_rows(x: torch.Tensor, row_idx: Optional[torch.Tensor] = None, q: Optio
     q = torch.empty((rows, Kp), dtype=torch.int8, device=dev) if q is None else q
     scale = torch.empty((rows,), dtype=torch.float32, device=dev) if scale is None else scale
     qp, sp = _like(q, (rows, Kp), torch.int8, dev, "q"), _like(scale, (rows,), torch.float32, dev, "scale")
-    with _on(x):
-        L.check(L.lib().oc_quant_rows(_DTYPES[x.dtype], at, ld, n, K, ip, rows, qp, sp, _stream_of(x)))
+    _call("oc_quant_rows", dev, _DTYPES[x.dtype], at, ld, n, K, ip, rows, qp, sp)
     return q, scale
 
 
@@ -309,7 +326,5 @@ def linear_i8(q: torch.Tensor, scale: torch.Tensor, w: torch.Tensor, w_scale: to
         raise _bad(L.OC_ERR_SHAPE, f"y is {tuple(y.shape)} {y.dtype} on {y.device}, expected [..., {N}] on {dev}")
     bp = _like(bias, (N,), y.dtype, dev, "bias")
     ip = _ids(out_idx, (rows,), dev, "out_idx")
-    with _on(q):
-        L.check(L.lib().oc_linear_i8(_DTYPES[y.dtype], rows, Kp, N, qp, sp, wp, swp, bp, L.ACTS[act], ip, y.shape[0],
-                                     at, ld, _stream_of(q)))
+    _call("oc_linear_i8", dev, _DTYPES[y.dtype], rows, Kp, N, qp, sp, wp, swp, bp, L.ACTS[act], ip, y.shape[0], at, ld)
     return y
