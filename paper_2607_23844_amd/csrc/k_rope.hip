@@ -1,12 +1,13 @@
 // Rotary positions of q and k rows with up to three axes.
 //
-// A thread owns one unit of a head's channels, the same for all heads of its
-// row: 8 neighbouring channels (pairs side by side), or V channels and their V
-// partners half a section further.  The cosines and sines of its pairs are
-// computed once and used for every head of q and k.  Angles: a position times
-// turns per position in 64 bits, less the whole turns, then cospi and sinpi of
-// a fp32 fraction of at most a half (positions of 2^20 would lose 2^-4 of a
-// turn in 32 bits).
+// A block turns `rows` rows.  First the cosines and sines of its rows' pairs, one
+// per thread, into LDS: a position times turns per position in 64 bits, less
+// the whole turns, then cospi and sinpi of a fp32 fraction of at most a half
+// (positions of 2^20 would lose 2^-4 of a turn in 32 bits).  Then all heads of
+// q and k of those rows, in units of 8 neighbouring channels (pairs side by
+// side) or of V channels and their V partners half a section further;
+// consecutive threads take consecutive units, four of them loaded at a time.
+// Bound by q's and k's way through HBM.
 #include "oc_attn_common.h"
 #include "oc_device.h"
 #include "oc_launch.h"
@@ -43,89 +44,105 @@ __device__ __forceinline__ void put(T *p, const float (&v)[V]) {
     *reinterpret_cast<C *>(p) = c;
 }
 
+constexpr int ROPE_ROWS = 16;   // most rows of a block
+struct Turn { float c, s; };
+
 // PAIRS: unit u is channels 8u..8u+7 (V = 4 pairs); else channels lo.. and hi.. of V pairs
 template <typename T, bool PAIRS, int V>
-__global__ __launch_bounds__(256) void k_rope(RopeGeom g, RopeArgs a) {
-    const int units = g.dh / 2 / V;
-    const long id = (long)folded_block() * 256 + threadIdx.x, row = id / units;
-    const int u = (int)(id - row * units), p0 = u * V;
-    if (row >= a.rows) return;
-    double at[3];
-    if (a.pos != nullptr) {
+__global__ __launch_bounds__(256) void k_rope(RopeGeom g, RopeArgs a, int block_rows) {
+    __shared__ __align__(16) Turn turns[ROPE_ROWS * ROPE_MAX_PAIRS];
+    __shared__ int where[ROPE_ROWS][4];   // position on the axes; whether there is one
+    const long row0 = (long)folded_block() * block_rows;
+    if (row0 >= a.rows) return;
+    const int rows = (int)min((long)block_rows, a.rows - row0);
+    if ((int)threadIdx.x < rows) {
+        const long row = row0 + threadIdx.x;
+        int *const w = where[threadIdx.x];
+        if (a.pos != nullptr) {
 #pragma unroll
-        for (int i = 0; i < 3; ++i) at[i] = a.pos[row * 3 + i];
-    } else {
-        const long t = batch_token((int)row, a.idx, a.tF, a.tN);
-        if (t < 0 || t >= g.FN) return;
-        const int f = (int)(t / g.N), n = (int)(t - (long)f * g.N);
-        at[0] = f;
-        at[1] = n / g.W;
-        at[2] = n % g.W;
-    }
-    float co[V], si[V];
-    bool on[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int p = p0 + j;
-        on[j] = p < g.P;
-        const int axis = p < g.axis1 ? 0 : p < g.axis2 ? 1 : 2;
-        const double pos = axis == 0 ? at[0] + g.origin[0] : axis == 1 ? at[1] + g.origin[1] : at[2] + g.origin[2];
-        const double t = on[j] ? pos * g.turn[p] : 0.0;
-        const float x = 2.f * (float)(t - rint(t));
-        co[j] = cospif(x);
-        si[j] = a.inverse ? -sinpif(x) : sinpif(x);
-    }
-    int lo = 2 * p0, hi = 0;
-    if constexpr (!PAIRS) {
-        int s0 = 0, s1 = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (p0 >= g.sect[i] && p0 < g.sect[i + 1]) {
-                s0 = g.sect[i];
-                s1 = g.sect[i + 1];
-            }
-        lo = s0 + p0;
-        hi = lo + (s1 - s0);
-    }
-    auto turn = [&](const T *src, T *dst) {
-        if constexpr (PAIRS) {
-            float v[8];
-            get<T, 8>(src + lo, v);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (!on[j]) continue;
-                const float x = v[2 * j], y = v[2 * j + 1];
-                v[2 * j] = fmaf(x, co[j], -(y * si[j]));
-                v[2 * j + 1] = fmaf(x, si[j], y * co[j]);
-            }
-            put<T, 8>(dst + lo, v);
+            for (int i = 0; i < 3; ++i) w[i] = a.pos[row * 3 + i];
+            w[3] = 1;
         } else {
-            float v[V], w[V];
-            get<T, V>(src + lo, v);
-            get<T, V>(src + hi, w);
+            const long t = batch_token((int)row, a.idx, a.tF, a.tN);
+            w[3] = t >= 0 && t < g.FN;
+            if (w[3]) {   // (fewer than 2^30 tokens)
+                const int f = (int)t / g.N, n = (int)t - f * g.N;
+                w[0] = f;
+                w[1] = n / g.W;
+                w[2] = n % g.W;
+            }
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < rows * g.P; e += 256) {
+        const int r = e / g.P, p = e - r * g.P, axis = p < g.axis1 ? 0 : p < g.axis2 ? 1 : 2;
+        const double t = ((double)where[r][axis] + g.origin[axis]) * g.turn[p];
+        const float x = 2.f * (float)(t - rint(t)), sn = sinpif(x);
+        turns[r * ROPE_MAX_PAIRS + p] = Turn{cospif(x), a.inverse ? -sn : sn};
+    }
+    __syncthreads();
+    const int units = g.dh / 2 / V, q_units = a.q != nullptr ? a.heads * units : 0;
+    const int row_units = q_units + (a.k != nullptr ? a.k_heads * units : 0);
+    constexpr int N = 4, W = PAIRS ? 8 : V;   // units at a time; channels of a run
+    for (int i0 = threadIdx.x; i0 < rows * row_units; i0 += 256 * N) {
+        float v[N][W], w[PAIRS ? 1 : N][W];
+        T *to[N];
+        int first[N], gap[N], of[N];
+#pragma unroll
+        for (int b = 0; b < N; ++b) {
+            const int i = i0 + b * 256, r = i / row_units;
+            to[b] = nullptr;
+            if (i >= rows * row_units || !where[r][3]) continue;
+            int j = i - r * row_units;
+            const bool k = j >= q_units;
+            if (k) j -= q_units;
+            const int h = j / units, p0 = (j - h * units) * V;
+            const long row = row0 + r;
+            const T *src = k ? (const T *)a.k + row * a.ld_k : (const T *)a.q + row * a.ld_q;
+            to[b] = k ? (T *)a.ko + row * a.ld_ko : (T *)a.qo + row * a.ld_qo;
+            int lo = 2 * p0;
+            if constexpr (!PAIRS) {
+                int s0 = 0, s1 = 0;
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+                    if (p0 >= g.sect[m] && p0 < g.sect[m + 1]) {
+                        s0 = g.sect[m];
+                        s1 = g.sect[m + 1];
+                    }
+                lo = s0 + p0;
+                gap[b] = s1 - s0;
+            }
+            src += h * g.dh + lo;
+            to[b] += h * g.dh + lo;
+            first[b] = p0;
+            of[b] = r * ROPE_MAX_PAIRS;
+            get<T, W>(src, v[b]);
+            if constexpr (!PAIRS) get<T, W>(src + gap[b], w[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < N; ++b) {
+            if (to[b] == nullptr) continue;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                if (!on[j]) continue;
-                const float x = v[j], y = w[j];
-                v[j] = fmaf(x, co[j], -(y * si[j]));
-                w[j] = fmaf(x, si[j], y * co[j]);
+                if (first[b] + j >= g.P) break;   // (not turned)
+                const Turn t = turns[of[b] + first[b] + j];
+                float &x = PAIRS ? v[b][2 * j] : v[b][j], &y = PAIRS ? v[b][2 * j + 1] : w[PAIRS ? 0 : b][j];
+                const float x0 = x, y0 = y;
+                x = fmaf(x0, t.c, -(y0 * t.s));
+                y = fmaf(x0, t.s, y0 * t.c);
             }
-            put<T, V>(dst + lo, v);
-            put<T, V>(dst + hi, w);
+            put<T, W>(to[b], v[b]);
+            if constexpr (!PAIRS) put<T, W>(to[b] + gap[b], w[b]);
         }
-    };
-    if (a.q != nullptr)
-        for (int h = 0; h < a.heads; ++h)
-            turn((const T *)a.q + row * a.ld_q + h * g.dh, (T *)a.qo + row * a.ld_qo + h * g.dh);
-    if (a.k != nullptr)
-        for (int h = 0; h < a.k_heads; ++h)
-            turn((const T *)a.k + row * a.ld_k + h * g.dh, (T *)a.ko + row * a.ld_ko + h * g.dh);
+    }
 }
 
 template <typename T, bool PAIRS, int V>
 hipError_t go_rope(const RopeGeom &g, const RopeArgs &a, hipStream_t st) {
-    const long threads = (long)a.rows * (g.dh / 2 / V);
-    launch_k(k_rope<T, PAIRS, V>, folded_grid((threads + 255) / 256, 256), 256, 0, st, g, a);
+    // rows of a block: all that leave two blocks for every unit
+    int rows = 1;
+    while (rows < ROPE_ROWS && a.rows / (2 * rows) >= 2 * N_CUS) rows *= 2;
+    launch_k(k_rope<T, PAIRS, V>, folded_grid((a.rows + rows - 1) / rows, 256), 256, 0, st, g, a, rows);
     return hipGetLastError();
 }
 
