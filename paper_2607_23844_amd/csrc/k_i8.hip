@@ -162,25 +162,31 @@ __device__ __forceinline__ float gelu_tanh(float v) {
     return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-2.8853900817779268f * z));
 }
 
-// Four consecutive outputs of a row from their sums.
+// Scales and biases of four consecutive outputs, and these outputs of a row from
+// their sums.
 template <typename T>
-__device__ __forceinline__ f32x4 finish4(const LinearI8Args &a, const int (&acc)[4], float sq, int n) {
-    const f32x4 sw = *reinterpret_cast<const f32x4 *>(a.sw + n);
+__device__ __forceinline__ void columns4(const LinearI8Args &a, int n, f32x4 &sw, f32x4 &b) {
+    sw = *reinterpret_cast<const f32x4 *>(a.sw + n);
+    b = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (a.bias == nullptr) return;
+    if constexpr (sizeof(T) == 2) {
+        const u16x4 h = *reinterpret_cast<const u16x4 *>((const uint16_t *)a.bias + n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = bf2f(h[e]);
+    } else {
+        b = *reinterpret_cast<const f32x4 *>((const float *)a.bias + n);
+    }
+}
+__device__ __forceinline__ i32x4 four(const i32x16 &acc, int g) {
+    return i32x4{acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]};
+}
+template <bool GELU>
+__device__ __forceinline__ f32x4 finish4(i32x4 acc, float sq, f32x4 sw, f32x4 b) {
     f32x4 v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = (float)acc[e] * sq * sw[e];
-    if (a.bias != nullptr) {
-        if constexpr (sizeof(T) == 2) {
-            const u16x4 b = *reinterpret_cast<const u16x4 *>((const uint16_t *)a.bias + n);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += bf2f(b[e]);
-        } else {
-            v += *reinterpret_cast<const f32x4 *>((const float *)a.bias + n);
-        }
-    }
-    if (a.gelu) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = gelu_tanh(v[e]);
+    for (int e = 0; e < 4; ++e) {
+        v[e] = fmaf((float)acc[e] * sq, sw[e], b[e]);
+        if constexpr (GELU) v[e] = gelu_tanh(v[e]);
     }
     return v;
 }
@@ -189,6 +195,12 @@ __device__ __forceinline__ u16x4 to_bf16(f32x4 v) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = (__bf16)v[e];
     return *reinterpret_cast<u16x4 *>(&o);
+}
+
+// Between a wave's writes and reads of LDS that no other wave touches.
+__device__ __forceinline__ void wave_lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 // y row of batch row r, or -1
@@ -201,10 +213,9 @@ __device__ __forceinline__ long out_row(const LinearI8Args &a, long r) {
 // ---------------------------------------------------------------------------
 // The product on ring-buffered MFMA tiles: a = weight rows, b = batch rows.
 // bf16 tiles are staged through LDS and written in 16-byte chunks of whole
-// rows; fp32 rows are stored as the accumulators hold them, four outputs at a
-// time.
+// rows, fp32 tiles wave by wave.
 // ---------------------------------------------------------------------------
-template <int ID, typename T>
+template <int ID, typename T, bool GELU>
 __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, int n_at, int n_bt) {
     using R = typename RingShape<ID, RING_I8>::Tile;
     constexpr int BA = R::BA, BB = R::BB;
@@ -219,34 +230,58 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, 
     ring_rows(rb, (const uint16_t *)a.q, a.rows, K2, b0);
     R t;
     t.run(lds, ra, rb, K2);
+    float sq[R::TB];
 #pragma unroll
-    for (int j = 0; j < R::TB; ++j) {
-        const int b = R::b_of(j);
-        const float sq = a.sq[min(b0 + b, a.rows - 1)];
-        T *to = nullptr;
-        if constexpr (sizeof(T) == 4) {
-            const long o = out_row(a, b0 + b);
-            if (o >= 0) to = (T *)a.y + o * a.ld_y;
-        }
+    for (int j = 0; j < R::TB; ++j) sq[j] = a.sq[min(b0 + R::b_of(j), a.rows - 1)];
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int i = 0; i < R::TA; ++i)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int n = R::a_of(i, g);
                 if (a0 + n >= a.N) continue;
-                const int acc[4] = {t.acc[i][j][4 * g], t.acc[i][j][4 * g + 1], t.acc[i][j][4 * g + 2],
-                                    t.acc[i][j][4 * g + 3]};
-                const f32x4 v = finish4<T>(a, acc, sq, a0 + n);
-                if constexpr (sizeof(T) == 2) *reinterpret_cast<u16x4 *>(lds + b * (BA + 8) + n) = to_bf16(v);
-                else if (to != nullptr) *reinterpret_cast<f32x4 *>(to + a0 + n) = v;
+                f32x4 sw, bias;
+                columns4<T>(a, a0 + n, sw, bias);
+#pragma unroll
+                for (int j = 0; j < R::TB; ++j)
+                    *reinterpret_cast<u16x4 *>(lds + R::b_of(j) * (BA + 8) + n) =
+                        to_bf16(finish4<GELU>(four(t.acc[i][j], g), sq[j], sw, bias));
             }
-    }
-    if constexpr (sizeof(T) == 2) {
         __syncthreads();
         write_rows<BA, BB, R::NT>(lds, min(BA, a.N - a0), [&](int b, int c0) -> uint16_t * {
             const long o = out_row(a, b0 + b);
             return o >= 0 ? (uint16_t *)a.y + o * a.ld_y + a0 + c0 : nullptr;
         });
+    } else {
+        // 32 rows of 32 outputs at a time through a part of LDS of the wave's own: 128 bytes of a row
+        // are stored together (each lane storing its four outputs took 80 us for 4429 x 1536 x 6144)
+        constexpr int LD = 36;
+        const int lane = threadIdx.x & 63;
+        float *const mine = reinterpret_cast<float *>(lds) + (threadIdx.x >> 6) * 32 * LD;
+        static_assert(R::NW * 32 * LD * 4 <= R::LDS_BYTES, "the waves' parts fit in the ring");
+#pragma unroll
+        for (int i = 0; i < R::TA; ++i) {
+            f32x4 sw[4], bias[4];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) columns4<T>(a, min(a0 + R::a_of(i, g), a.N - 4), sw[g], bias[g]);
+            const int n = a0 + (R::a_of(i, 0) & ~31) + (lane & 7) * 4;   // outputs that this lane stores
+#pragma unroll
+            for (int j = 0; j < R::TB; ++j) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *reinterpret_cast<f32x4 *>(mine + (lane & 31) * LD + 8 * g + 4 * (lane >> 5)) =
+                        finish4<GELU>(four(t.acc[i][j], g), sq[j], sw[g], bias[g]);
+                wave_lds_fence();
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int r = k * 8 + (lane >> 3);
+                    const f32x4 v = *reinterpret_cast<const f32x4 *>(mine + r * LD + (lane & 7) * 4);
+                    const long o = out_row(a, b0 + (R::b_of(j) & ~31) + r);
+                    if (o >= 0 && n < a.N) *reinterpret_cast<f32x4 *>((T *)a.y + o * a.ld_y + n) = v;
+                }
+                wave_lds_fence();
+            }
+        }
     }
 }
 
@@ -299,8 +334,9 @@ __global__ __launch_bounds__(1024) void k_linear_i8_thin(LinearI8Args a) {
         if (o < 0 || n0 + n >= a.N) continue;
         i32x4 s = zero;
         for (int v = 0; v < nw; ++v) s += *reinterpret_cast<const i32x4 *>(part + (v * RT * 16 + r) * LD + n);
-        const int sum[4] = {s[0], s[1], s[2], s[3]};
-        const f32x4 f = finish4<T>(a, sum, a.sq[r], n0 + n);
+        f32x4 sw, bias;
+        columns4<T>(a, n0 + n, sw, bias);
+        const f32x4 f = a.gelu ? finish4<true>(s, a.sq[r], sw, bias) : finish4<false>(s, a.sq[r], sw, bias);
         T *const to = (T *)a.y + o * a.ld_y + n0 + n;
         if constexpr (sizeof(T) == 2) *reinterpret_cast<u16x4 *>(to) = to_bf16(f);
         else *reinterpret_cast<f32x4 *>(to) = f;
@@ -318,6 +354,21 @@ hipError_t go_thin(const LinearI8Args &a, hipStream_t st) {
     return hipGetLastError();
 }
 
+template <typename T, bool GELU>
+hipError_t go_ring(const LinearI8Args &a, hipStream_t st) {
+    const int K2 = (int)(i8_row(a.K) / 2);
+    const int id = ring_pick(K2, [&](int BA, int BB) { return (long)cdiv(a.N, BA) * cdiv(a.rows, BB); });
+    return ring_dispatch(id, [&](auto c) -> hipError_t {
+        constexpr int ID = decltype(c)::value;
+        using R = typename RingShape<ID, RING_I8>::Tile;
+        const hipError_t e = allow_lds(k_linear_i8<ID, T, GELU>, R::LDS_BYTES);
+        if (e != hipSuccess) return e;
+        const int n_at = cdiv(a.N, R::BA), n_bt = cdiv(a.rows, R::BB);
+        launch_k(k_linear_i8<ID, T, GELU>, (unsigned)(n_at * n_bt), R::NT, R::LDS_BYTES, st, a, n_at, n_bt);
+        return hipGetLastError();
+    });
+}
+
 template <typename T>
 hipError_t go_linear(const LinearI8Args &a, hipStream_t st) {
     // Up to 16 rows: 3.9 us against the ring's 6.7 for one row of K = N = 1536, 6.3 against 8.5 at N =
@@ -325,17 +376,7 @@ hipError_t go_linear(const LinearI8Args &a, hipStream_t st) {
     // against 6.8, N = 4608 7.3 against 7.0 (every block reads all rows from L2).
     if (a.rows <= 16) return go_thin<T, 1>(a, st);
     if (a.rows <= 32 && a.N <= 4096) return go_thin<T, 2>(a, st);
-    const int K2 = (int)(i8_row(a.K) / 2);
-    const int id = ring_pick(K2, [&](int BA, int BB) { return (long)cdiv(a.N, BA) * cdiv(a.rows, BB); });
-    return ring_dispatch(id, [&](auto c) -> hipError_t {
-        constexpr int ID = decltype(c)::value;
-        using R = typename RingShape<ID, RING_I8>::Tile;
-        const hipError_t e = allow_lds(k_linear_i8<ID, T>, R::LDS_BYTES);
-        if (e != hipSuccess) return e;
-        const int n_at = cdiv(a.N, R::BA), n_bt = cdiv(a.rows, R::BB);
-        launch_k(k_linear_i8<ID, T>, (unsigned)(n_at * n_bt), R::NT, R::LDS_BYTES, st, a, n_at, n_bt);
-        return hipGetLastError();
-    });
+    return a.gelu ? go_ring<T, true>(a, st) : go_ring<T, false>(a, st);
 }
 
 }  // namespace

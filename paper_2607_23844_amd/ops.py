@@ -146,10 +146,16 @@ def norm_gate(x: torch.Tensor, shape: Shape, y: Optional[torch.Tensor] = None, p
         if h is not None and h is not False:
             raise _bad(L.OC_ERR_INVALID_ARG, "h is x where y is None")
         h = False
-    h = torch.empty_like(x) if h is None else h
-    n = torch.empty_like(x) if n is None else n
-    hp = None if h is False else _like(h, full, dt, dev, "h")
-    np_ = None if n is False else _like(n, full, dt, dev, "n")
+    if h is None:
+        h = torch.empty_like(x)
+        hp = h.data_ptr()
+    else:
+        hp = None if h is False else _like(h, full, dt, dev, "h")
+    if n is None:
+        n = torch.empty_like(x)
+        np_ = n.data_ptr()
+    else:
+        np_ = None if n is False else _like(n, full, dt, dev, "n")
     po, pr, mo = _norm(post, shape, dev, "post"), _norm(pre, shape, dev, "pre"), _mod(mod, rows, shape, dev)
     if rows == 0:      # (empty tensors have no address)
         hp = np_ = xp = yp = None
@@ -291,9 +297,16 @@ def quant_rows(x: torch.Tensor, row_idx: Optional[torch.Tensor] = None, q: Optio
     rows = n if row_idx is None else row_idx.numel()
     ip = _ids(row_idx, (rows,), dev, "row_idx")
     Kp = (K + 15) // 16 * 16
-    q = torch.empty((rows, Kp), dtype=torch.int8, device=dev) if q is None else q
-    scale = torch.empty((rows,), dtype=torch.float32, device=dev) if scale is None else scale
-    qp, sp = _like(q, (rows, Kp), torch.int8, dev, "q"), _like(scale, (rows,), torch.float32, dev, "scale")
+    if q is None:
+        q = torch.empty((rows, Kp), dtype=torch.int8, device=dev)
+        qp = q.data_ptr()
+    else:
+        qp = _like(q, (rows, Kp), torch.int8, dev, "q")
+    if scale is None:
+        scale = torch.empty((rows,), dtype=torch.float32, device=dev)
+        sp = scale.data_ptr()
+    else:
+        sp = _like(scale, (rows,), torch.float32, dev, "scale")
     _call("oc_quant_rows", dev, _DTYPES[x.dtype], at, ld, n, K, ip, rows, qp, sp)
     return q, scale
 
