@@ -10,6 +10,7 @@
 // (sums over the rows that share the vector, means over the channels).
 #include "oc_device.h"
 #include "oc_launch.h"
+#include "oc_norm_plan.h"
 #include "oc_ops.h"
 #include "oc_attn_common.h"
 #include <algorithm>
@@ -851,10 +852,6 @@ __global__ void k_zero(float *p, int n) {
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) p[i] = 0.f;
 }
 
-size_t up256(size_t b) { return (b + 255) & ~(size_t)255; }
-
-int wide_part(int rows) { return std::max(1, cdiv(rows, 1024)); }
-
 }  // namespace
 
 hipError_t launch_zero(float *p, int n, hipStream_t st) {
@@ -862,38 +859,38 @@ hipError_t launch_zero(float *p, int n, hipStream_t st) {
     return hipGetLastError();
 }
 
-// f(threads per row, chunks of 8 channels per thread) for a row of C channels;
-// (256, 0): too long for registers.  The fewest lanes that hold a row in three
-// chunks (four from 1537 channels) where there are rows for all units: fewer
-// lanes idle and fewer steps in a sum; else the block.
+// f(threads per row, chunks per thread) of a team as constants
 template <typename F>
-static hipError_t norm_shape(int rows, int C, F f) {
+static hipError_t with_team(NormTeam t, F f) {
     using std::integral_constant;
-    const int c = cdiv(C, 8);
-    if (c <= 256 && rows >= 4 * N_CUS) {
-        constexpr integral_constant<int, 16> quarter{};
-        constexpr integral_constant<int, 32> half{};
-        constexpr integral_constant<int, 64> wave{};
-        constexpr integral_constant<int, 1> one{};
-        constexpr integral_constant<int, 2> two{};
-        constexpr integral_constant<int, 3> three{};
-        if (c <= 16) return f(quarter, one);
-        if (c <= 32) return f(quarter, two);
-        if (c <= 48) return f(quarter, three);
-        if (c <= 64) return f(half, two);
-        if (c <= 96) return f(half, three);
-        if (c <= 128) return f(wave, two);
-        return c <= 192 ? f(wave, three) : f(wave, integral_constant<int, 4>{});
-    }
+    constexpr integral_constant<int, 16> quarter{};
+    constexpr integral_constant<int, 32> half{};
+    constexpr integral_constant<int, 64> wave{};
     constexpr integral_constant<int, 256> block{};
-    if (c <= 256) return f(block, integral_constant<int, 1>{});
-    if (c <= 512) return f(block, integral_constant<int, 2>{});
-    return c <= 1024 ? f(block, integral_constant<int, 4>{}) : f(block, integral_constant<int, 0>{});
+    constexpr integral_constant<int, 1> one{};
+    constexpr integral_constant<int, 2> two{};
+    constexpr integral_constant<int, 3> three{};
+    constexpr integral_constant<int, 4> four{};
+    switch (t.threads * 8 + t.chunks) {
+        case 16 * 8 + 1: return f(quarter, one);
+        case 16 * 8 + 2: return f(quarter, two);
+        case 16 * 8 + 3: return f(quarter, three);
+        case 32 * 8 + 2: return f(half, two);
+        case 32 * 8 + 3: return f(half, three);
+        case 64 * 8 + 2: return f(wave, two);
+        case 64 * 8 + 3: return f(wave, three);
+        case 64 * 8 + 4: return f(wave, four);
+        case 256 * 8 + 1: return f(block, one);
+        case 256 * 8 + 2: return f(block, two);
+        case 256 * 8 + 4: return f(block, four);
+        case 256 * 8: return f(block, integral_constant<int, 0>{});
+        default: return hipErrorInvalidValue;
+    }
 }
 
 template <typename T>
 static hipError_t go_norm_gate(const NormArgs &a, T *h, T *n, hipStream_t st) {
-    return norm_shape(a.rows, a.C, [&](auto tpr, auto ch) -> hipError_t {
+    return with_team(norm_team(a.rows, a.C), [&](auto tpr, auto ch) -> hipError_t {
         constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
         if constexpr (CH == 0)
             launch_k(k_norm_gate_wide<T>, folded_grid(a.rows, 256), 256, 0, st, a, h, n);
@@ -908,120 +905,65 @@ hipError_t launch_norm_gate(const NormArgs &a, void *h, void *n, hipStream_t st)
     return a.bf16 ? go_norm_gate(a, (uint16_t *)h, (uint16_t *)n, st) : go_norm_gate(a, (float *)h, (float *)n, st);
 }
 
-// (512 blocks: 230400 x 320 210 us and 30000 x 1536 127 against 224 and 136 with 1024, whose partial sums
-// weigh more; 256: 205 and 124, but 71 against 56 at 230400 x 64)
-constexpr int GRAD_BLOCKS = 512;
+static_assert(sizeof(RowStats) == GRAD_ROW_STATS, "the plan's statistics");
 
-// Whether a team takes the rows of a modulation row alone, and the items of a
-// gradient call by blocks of `teams` teams.
-static bool grad_alone(int rows, int rows_per_mod, int teams) {
-    return teams > 1 && std::min(rows_per_mod, rows) < std::max(2 * teams, 16);
-}
-static GradItems grad_items(int rows, int rows_per_mod, int teams, int &blocks) {
-    GradItems g{};
-    const int per = std::min(rows_per_mod, rows), n_mod = cdiv(rows, per);
-    const bool alone = grad_alone(rows, rows_per_mod, teams);
-    // (an item's sums cost its share of LDS and of the join: four rows a team where that leaves no unit idle)
-    const int least = std::min(std::max(rows / (N_CUS * teams), 1), 4) * teams;
-    g.per_group = alone ? 1 : std::min(std::max(1, GRAD_BLOCKS / n_mod), cdiv(per, least));
-    g.part = cdiv(per, g.per_group);
-    g.per_group = cdiv(per, g.part);
-    g.n_items = n_mod * g.per_group;
-    blocks = std::min(alone ? cdiv(g.n_items, teams) : g.n_items, GRAD_BLOCKS);
-    return g;
-}
-
-// enough for every kernel choice: slots of at most GRAD_BLOCKS items (more only where each is a whole
-// modulation row and needs none) and sums of as many blocks; the long rows' statistics and parts
 size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod) {
-    if (rows <= 0) return 0;
-    const size_t items = std::min(rows, GRAD_BLOCKS);
-    const size_t wide = C > 8192 ? up256((size_t)rows * sizeof(RowStats)) : 0;
-    return wide + up256((rows_per_mod > 0 ? 6 : 0) * items * C * 4) + up256(4 * items * C * 4);
+    return rows > 0 ? grad_plan(rows, C, rows_per_mod > 0 ? rows_per_mod : rows, rows_per_mod > 0, true).bytes() : 0;
 }
 
 template <typename T, int TPR, int CH, bool SUMS, bool ALONE>
-static hipError_t go_norm_grad(const NormArgs &a, const T *dh, const T *dn, T *dx, T *dy, const NormGrads &q, void *ws,
-                               hipStream_t st) {
+static hipError_t go_norm_grad(const NormArgs &a, const T *dh, const T *dn, T *dx, T *dy, const NormGrads &q,
+                               const GradPlan &p, void *ws, hipStream_t st) {
     constexpr int TEAMS = Team<TPR>::PER_BLOCK, CP = TPR * CH * 8;
-    int blocks = 0;
-    GradItems g = grad_items(a.rows, a.rows_per_mod, TEAMS, blocks);
-    float *const out[N_Q] = {q.gate, q.scale, q.shift, q.post_w, q.post_b, q.pre_w, q.pre_b};
-    std::copy(out, out + N_Q, g.out);
-    const bool mods = q.gate || q.scale || q.shift, vecs = q.post_w || q.post_b || q.pre_w || q.pre_b;
-    g.slots = (float *)ws;
-    const size_t slots = mods && g.per_group > 1 ? 3 * (size_t)g.n_items * a.C * 4 : 0;
-    g.sums = (float *)((char *)ws + up256(slots));
+    GradItems g{{q.gate, q.scale, q.shift, q.post_w, q.post_b, q.pre_w, q.pre_b}, (float *)ws,
+                (float *)((char *)ws + p.slots), p.part, p.per_group, p.n_items};
     const size_t lds = ((ALONE ? 0 : 3) + (SUMS && (ALONE || TEAMS > 1) ? TEAMS : 0)) * (size_t)CP * 4;
     const hipError_t e = raise_lds_limit((const void *)k_norm_grad<T, TPR, CH, SUMS, ALONE>, lds);
     if (e != hipSuccess) return e;
-    launch_k(k_norm_grad<T, TPR, CH, SUMS, ALONE>, blocks, 256, lds, st, a, dh, dn, dx, dy, g);
-    if (slots > 0 || vecs)
-        launch_k(k_norm_grad_join, dim3((unsigned)cdiv(a.C, 64), slots > 0 ? (unsigned)(g.n_items / g.per_group) : 1u, N_Q),
-                 1024, 0, st, a.C, blocks, g);
+    launch_k(k_norm_grad<T, TPR, CH, SUMS, ALONE>, p.blocks, 256, lds, st, a, dh, dn, dx, dy, g);
+    if (p.slots > 0 || p.sums > 0)
+        launch_k(k_norm_grad_join,
+                 dim3((unsigned)cdiv(a.C, 64), p.slots > 0 ? (unsigned)(p.n_items / p.per_group) : 1u, N_Q), 1024, 0, st,
+                 a.C, p.blocks, g);
     return hipGetLastError();
 }
 
 template <typename T>
 static hipError_t go_norm_grad_wide(const NormArgs &a, const T *dh, const T *dn, T *dx, T *dy, const NormGrads &q,
-                                    void *ws, hipStream_t st) {
+                                    const GradPlan &p, void *ws, hipStream_t st) {
     RowStats *rows = (RowStats *)ws;
-    ColOut o{{q.gate, q.scale, q.shift, q.post_w, q.post_b, q.pre_w, q.pre_b}, nullptr, nullptr, 0, 0};
-    o.part = wide_part(a.rows);
-    o.n_parts = cdiv(a.rows, o.part);
-    const bool mods = q.gate || q.scale || q.shift, vecs = q.post_w || q.post_b || q.pre_w || q.pre_b;
-    char *w = (char *)ws + up256((size_t)a.rows * sizeof(RowStats));
-    o.slots = (float *)w;
-    o.sums = (float *)(w + up256((mods ? 6 : 0) * (size_t)o.n_parts * a.C * 4));
+    const ColOut o{{q.gate, q.scale, q.shift, q.post_w, q.post_b, q.pre_w, q.pre_b}, (float *)((char *)ws + p.stats),
+                   (float *)((char *)ws + p.stats + p.slots), p.part, p.n_items};
     launch_k(k_norm_grad_rows_wide<T>, folded_grid(a.rows, 256), 256, 0, st, a, dh, dn, dx, dy, rows);
-    if (!mods && !vecs) return hipGetLastError();
+    if (p.slots == 0 && p.sums == 0) return hipGetLastError();
     launch_k(k_norm_grad_cols_wide<T>, dim3((unsigned)o.n_parts, (unsigned)cdiv(a.C, 512)), 64, 0, st, a, dh, dn, rows, o);
     launch_k(k_norm_grad_join_wide, dim3((unsigned)o.n_parts, (unsigned)cdiv(a.C, 64), N_Q), 64, 0, st, a.C, a.rows,
              a.rows_per_mod, o);
     return hipGetLastError();
 }
 
-// As norm_shape, in two chunks where it can (a row's values, gradients and sums
-// take over 12 registers a channel).
-template <typename F>
-static hipError_t grad_shape(int rows, int C, F f) {
-    using std::integral_constant;
-    const int c = cdiv(C, 8);
-    constexpr integral_constant<int, 1> one{};
-    constexpr integral_constant<int, 2> two{};
-    if (c <= 256 && rows >= 4 * N_CUS) {
-        constexpr integral_constant<int, 16> quarter{};
-        constexpr integral_constant<int, 32> half{};
-        constexpr integral_constant<int, 64> wave{};
-        if (c <= 16) return f(quarter, one);
-        if (c <= 32) return f(quarter, two);
-        if (c <= 48) return f(quarter, integral_constant<int, 3>{});
-        if (c <= 64) return f(half, two);
-        if (c <= 128) return f(wave, two);
-        if (c <= 192) return f(wave, integral_constant<int, 3>{});
-    }
-    constexpr integral_constant<int, 256> block{};
-    if (c <= 256) return f(block, one);
-    if (c <= 512) return f(block, two);
-    return c <= 1024 ? f(block, integral_constant<int, 4>{}) : f(block, integral_constant<int, 0>{});
-}
-
 template <typename T>
 static hipError_t type_norm_grad(const NormArgs &a, const T *dh, const T *dn, T *dx, T *dy, const NormGrads &q,
                                  void *ws, hipStream_t st) {
     const bool mods = q.gate || q.scale || q.shift, vecs = q.post_w || q.post_b || q.pre_w || q.pre_b;
-    return grad_shape(a.rows, a.C, [&](auto tpr, auto ch) -> hipError_t {
+    const GradPlan p = grad_plan(a.rows, a.C, a.rows_per_mod, mods, vecs);
+    return with_team(p.team, [&](auto tpr, auto ch) -> hipError_t {
         constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
         if constexpr (CH == 0) {
-            return go_norm_grad_wide(a, dh, dn, dx, dy, q, ws, st);
+            return go_norm_grad_wide(a, dh, dn, dx, dy, q, p, ws, st);
         } else {
-            if constexpr (TPR < 256) {
-                if (grad_alone(a.rows, a.rows_per_mod, Team<TPR>::PER_BLOCK))
-                    return mods || vecs ? go_norm_grad<T, TPR, CH, true, true>(a, dh, dn, dx, dy, q, ws, st)
-                                        : go_norm_grad<T, TPR, CH, false, true>(a, dh, dn, dx, dy, q, ws, st);
+            // (teams that the plan takes: 32 lanes with three chunks and 64 with four are the forward's)
+            if constexpr ((TPR == 32 && CH == 3) || (TPR == 64 && CH == 4)) {
+                return hipErrorInvalidValue;
+            } else {
+                if constexpr (TPR < 256) {
+                    if (p.alone)
+                        return mods || vecs ? go_norm_grad<T, TPR, CH, true, true>(a, dh, dn, dx, dy, q, p, ws, st)
+                                            : go_norm_grad<T, TPR, CH, false, true>(a, dh, dn, dx, dy, q, p, ws, st);
+                }
+                return mods || vecs ? go_norm_grad<T, TPR, CH, true, false>(a, dh, dn, dx, dy, q, p, ws, st)
+                                    : go_norm_grad<T, TPR, CH, false, false>(a, dh, dn, dx, dy, q, p, ws, st);
             }
-            return mods || vecs ? go_norm_grad<T, TPR, CH, true, false>(a, dh, dn, dx, dy, q, ws, st)
-                                : go_norm_grad<T, TPR, CH, false, false>(a, dh, dn, dx, dy, q, ws, st);
         }
     });
 }

@@ -1,0 +1,91 @@
+// How norms share out their rows: teams of threads, and the items and workspace
+// of a gradient call.  Host only; everything follows from the sizes.
+#pragma once
+#include <algorithm>
+#include <cstddef>
+
+namespace oc {
+
+constexpr int NORM_CUS = 256;   // compute units
+
+// Threads of a row (16, 32, 64 or the block of 256) and chunks of 8 channels of
+// each; chunks 0: rows too long for registers.
+struct NormTeam { int threads, chunks; };
+
+// Forward: the fewest lanes that hold a row in three chunks (four from 1537
+// channels) where there are rows for all units, so that fewer lanes idle and
+// sums take fewer steps (230400 x 64: 29 us by 16 lanes, 94 by 64); else the
+// block, whose threads have less to do one after another.
+inline NormTeam norm_team(int rows, int C) {
+    const int c = (C + 7) / 8;
+    if (c <= 256 && rows >= 4 * NORM_CUS) {
+        if (c <= 48) return {16, (c + 15) / 16};
+        if (c <= 96) return {32, (c + 31) / 32};
+        return {64, (c + 63) / 64};
+    }
+    if (c <= 256) return {256, 1};
+    return {256, c <= 512 ? 2 : c <= 1024 ? 4 : 0};
+}
+
+// Gradients: in two chunks where 16, 32 or 64 lanes can hold that (a row's
+// values, gradients and sums take over 12 registers a channel; 230400 x 320:
+// 239 us by 16 lanes of three chunks, 282 by 32 of two), the block from 1537.
+inline NormTeam grad_team(int rows, int C) {
+    const int c = (C + 7) / 8;
+    if (c <= 192 && rows >= 4 * NORM_CUS) {
+        if (c <= 48) return {16, (c + 15) / 16};
+        if (c <= 64) return {32, 2};
+        return {64, c <= 128 ? 2 : 3};
+    }
+    if (c <= 256) return {256, 1};
+    return {256, c <= 512 ? 2 : c <= 1024 ? 4 : 0};
+}
+
+// Most blocks of a gradient call (512: 230400 x 320 210 us and 30000 x 1536 127
+// against 224 and 136 with 1024, whose partial sums weigh more; 256: 205 and
+// 124, but 71 against 56 at 230400 x 64).
+constexpr int GRAD_BLOCKS = 512;
+
+// Item i of n_items: rows [start, start + part) of modulation row i / per_group,
+// part i % per_group of it.  alone: a team takes an item by itself, else the
+// block's teams share it.  Rows too long for registers: n_items parts of all
+// rows instead.  Workspace: the rows' statistics (long rows), modulation sums
+// of the items (3 each; 6 for long rows' parts, which may cross two modulation
+// rows), sums of the blocks (4 each).
+struct GradPlan {
+    NormTeam team;
+    bool alone;
+    int part, per_group, n_items, blocks;
+    size_t stats, slots, sums;   // bytes, multiples of 256
+    size_t bytes() const { return stats + slots + sums; }
+};
+constexpr size_t GRAD_ROW_STATS = 24;   // bytes of a long row's statistics
+
+inline GradPlan grad_plan(int rows, int C, int rows_per_mod, bool mods, bool vecs) {
+    auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
+    auto div = [](int a, int b) { return (a + b - 1) / b; };
+    GradPlan g{};
+    g.team = grad_team(rows, C);
+    if (g.team.chunks == 0) {
+        g.part = div(rows, GRAD_BLOCKS);
+        g.per_group = 1;
+        g.n_items = g.blocks = div(rows, g.part);
+        g.stats = up((size_t)rows * GRAD_ROW_STATS);
+        g.slots = mods ? up(6 * (size_t)g.n_items * C * 4) : 0;
+    } else {
+        const int teams = 256 / g.team.threads, per = std::min(rows_per_mod, rows), n_mod = div(rows, per);
+        g.alone = teams > 1 && per < std::max(2 * teams, 16);
+        // (an item's sums cost its share of LDS and of the join: four rows a team where that leaves no unit idle)
+        const int least = std::min(std::max(rows / (NORM_CUS * teams), 1), 4) * teams;
+        g.per_group = g.alone ? 1 : std::min(std::max(1, GRAD_BLOCKS / n_mod), div(per, least));
+        g.part = div(per, g.per_group);
+        g.per_group = div(per, g.part);
+        g.n_items = n_mod * g.per_group;
+        g.blocks = std::min(g.alone ? div(g.n_items, teams) : g.n_items, GRAD_BLOCKS);
+        g.slots = mods && g.per_group > 1 ? up(3 * (size_t)g.n_items * C * 4) : 0;
+    }
+    g.sums = vecs ? up(4 * (size_t)g.blocks * C * 4) : 0;
+    return g;
+}
+
+}  // namespace oc

@@ -64,6 +64,19 @@ CASES = [
     (130, 136, torch.float32, dict(pre="none", post="none", per=64)),
     (40, 136, torch.bfloat16, dict(pre="none", post="rms")),
     (20000, 40, torch.bfloat16, dict(per=3, affine=True)),
+    # many rows: every team of lanes, with modulation rows that share items, fill them and are taken alone
+    (1100, 200, torch.float32, dict(per=300, affine=True, post="rms")),
+    (1100, 320, torch.bfloat16, dict(per=1100, affine=True, post="layer", rs=0.5)),
+    (1501, 320, torch.float32, dict(per=5, affine=True, post="rms")),
+    (1100, 408, torch.bfloat16, dict(per=37, post="rms", pre="rms")),
+    (1300, 704, torch.float32, dict(per=650, affine=True)),
+    (1030, 1000, torch.bfloat16, dict(per=1, affine=True, post="rms")),
+    (1030, 1000, torch.float32, dict(per=17, post="layer")),
+    (1100, 1536, torch.bfloat16, dict(per=9, affine=True, post="rms")),
+    (2100, 1536, torch.float32, dict(per=700, affine=True, post="rms")),
+    (1030, 2000, torch.bfloat16, dict(per=515, affine=True, post="layer")),
+    (4, 64, torch.float32, dict(per=3, affine=True, post="rms")),
+    (600, 8200, torch.bfloat16, dict(per=250, affine=True, post="rms")),
 ]
 IDS = [f"{r}x{c}-{str(t)[6:]}-{i}" for i, (r, c, t, _) in enumerate(CASES)]
 

@@ -300,3 +300,8 @@ def test_i8_rows_and_empty_calls():
         oc.quant_rows(torch.zeros(2, 64))
     with pytest.raises(oc.OmniCacheError):
         oc.linear_i8(*(torch.zeros(2, 64, dtype=torch.int8), torch.zeros(2)) * 2)
+
+
+def test_norm_gradient_plan_covers_its_rows_and_workspace(native):
+    r = native("norm_plan")()
+    assert r.returncode == 0, r.stdout[:2000]
