@@ -306,13 +306,6 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
                     raw[i].v[k] = reinterpret_cast<const uint4 *>(p + at + r.at(i))[k];
             }
     };
-    auto fetch_row = [&](long row) {
-        const long at = row * a.C;
-        fetch((const T *)a.y, at, ry);
-        fetch((const T *)a.x, at, rx);
-        fetch(dn, at, rn);
-        fetch(dh, at, rh);
-    };
     const int first = ALONE ? (int)blockIdx.x * TEAMS + team : (int)blockIdx.x;
     const int items = (int)gridDim.x * (ALONE ? TEAMS : 1);
     constexpr int STEP = ALONE ? 1 : TEAMS;
@@ -323,7 +316,12 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
         const long stop = min(min(start + g.part, (long)(group + 1) * a.rows_per_mod), (long)a.rows);
         const long mod = group * a.ld;
         long row = start + (ALONE ? 0 : team);
-        if (row < stop) fetch_row(row);
+        if (row < stop) {
+            fetch((const T *)a.y, row * a.C, ry);
+            fetch((const T *)a.x, row * a.C, rx);
+            fetch(dn, row * a.C, rn);
+            fetch(dh, row * a.C, rh);
+        }
         if constexpr (ALONE) {
 #pragma unroll
             for (int i = 0; i < CH; ++i)
@@ -347,16 +345,18 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
         }
         while (row < stop) {
             const long at = row * a.C;
-            Vals u, v, t, H;
+            Vals u, v, t;
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 widen(ry[i], v[i]);
                 widen(rx[i], u[i]);
-                widen(rn[i], t[i]);
-                widen(rh[i], H[i]);
             }
             row += STEP;
-            if (row < stop) fetch_row(row);
+            const long next = row * a.C;
+            if (row < stop) {
+                fetch((const T *)a.y, next, ry);
+                fetch((const T *)a.x, next, rx);
+            }
             float r_y = 1.f;
             if (a.y != nullptr) {
                 r_y = r.normalise(a.post, a.post_eps, v, red);
@@ -375,6 +375,7 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
             for (int i = 0; i < CH; ++i) {
                 float R[8];
                 cst(2, i, R);
+                widen(rn[i], t[i]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if constexpr (SUMS) {
@@ -386,20 +387,26 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
                     s2 = fmaf(t[i][e], u[i][e], s2);
                 }
             }
+            if (row < stop) fetch(dn, next, rn);
             float m1 = 0.f, m2 = 0.f;
             if (a.pre != 0) {
                 Team<TPR>::sum2(s1, s2, red);
                 m1 = a.pre == NORM_LAYER ? s1 * per_c : 0.f;
                 m2 = s2 * per_c;
             }
+            // t becomes H
 #pragma unroll
-            for (int i = 0; i < CH; ++i)
+            for (int i = 0; i < CH; ++i) {
+                float o[8];
+                widen(rh[i], o);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    H[i][e] = fmaf(r_h, fmaf(-u[i][e], m2, t[i][e] - m1), H[i][e]);
-                    u[i][e] = rs * H[i][e];
+                    t[i][e] = fmaf(r_h, fmaf(-u[i][e], m2, t[i][e] - m1), o[e]);
+                    o[e] = rs * t[i][e];
                 }
-            if (dx != nullptr) r.store(dx + at, u);
+                if (dx != nullptr && r.in(i)) store8(dx + at + r.at(i), o);
+            }
+            if (row < stop) fetch(dh, next, rh);
             if (a.y == nullptr) continue;
             s1 = s2 = 0.f;
 #pragma unroll
@@ -409,12 +416,12 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if constexpr (SUMS) {
-                        sum[2][i][e] = fmaf(H[i][e], v[i][e], sum[2][i][e]);
-                        sum[3][i][e] += H[i][e];
+                        sum[2][i][e] = fmaf(t[i][e], v[i][e], sum[2][i][e]);
+                        sum[3][i][e] += t[i][e];
                     }
-                    H[i][e] *= P[e];
-                    s1 += H[i][e];
-                    s2 = fmaf(H[i][e], v[i][e], s2);
+                    t[i][e] *= P[e];
+                    s1 += t[i][e];
+                    s2 = fmaf(t[i][e], v[i][e], s2);
                 }
             }
             if (dy == nullptr) continue;
@@ -424,9 +431,9 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) H[i][e] = r_y * fmaf(-v[i][e], k2, H[i][e] - k1);
+                    for (int e = 0; e < 8; ++e) t[i][e] = r_y * fmaf(-v[i][e], k2, t[i][e] - k1);
             }
-            r.store(dy + at, H);
+            r.store(dy + at, t);
         }
         if constexpr (SUMS) {
             // the sums of N channels from c on, to the gradients that they make
