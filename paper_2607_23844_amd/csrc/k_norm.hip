@@ -57,6 +57,24 @@ __device__ __forceinline__ void load8_or(const T *p, long at, float other, float
     }
 }
 
+// the same of four or eight elements
+template <int N, typename T>
+__device__ __forceinline__ void load_or(const T *p, long at, float other, float (&v)[N]) {
+    static_assert(N == 4 || N == 8, "chunks of four or eight");
+    if constexpr (N == 8) {
+        load8_or(p, at, other, v);
+    } else if (p == nullptr) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = other;
+    } else if constexpr (sizeof(T) == 2) {
+        const u16x4 w = *reinterpret_cast<const u16x4 *>(p + at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = bf2f(w[i]);
+    } else {
+        *reinterpret_cast<f32x4 *>(v) = *reinterpret_cast<const f32x4 *>(p + at);
+    }
+}
+
 // Sum over the block's 256 threads, the same order for every thread.
 __device__ __forceinline__ float block_sum(float v, float *red) {
     v = wave_sum(v);
@@ -306,6 +324,7 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
                     raw[i].v[k] = reinterpret_cast<const uint4 *>(p + at + r.at(i))[k];
             }
     };
+    const bool vecs = g.out[Q_POSTW] || g.out[Q_POSTB] || g.out[Q_PREW] || g.out[Q_PREB];
     const int first = ALONE ? (int)blockIdx.x * TEAMS + team : (int)blockIdx.x;
     const int items = (int)gridDim.x * (ALONE ? TEAMS : 1);
     constexpr int STEP = ALONE ? 1 : TEAMS;
@@ -439,19 +458,18 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
             // the sums of N channels from c on, to the gradients that they make
             auto emit = [&](int c, auto width, const float *sa, const float *sb, const float *sc, const float *sd) {
                 constexpr int N = decltype(width)::value;
-                auto vector = [&](const void *p, long at, float other, float (&v)[N]) {
-#pragma unroll
-                    for (int e = 0; e < N; ++e) v[e] = p != nullptr ? Elem<T>::ld((const T *)p + at + e) : other;
-                };
-                float w[N], b[N], m[N], o[3][N];
-                vector(a.post_w, c, 1.f, w);
-                vector(a.post_b, c, 0.f, b);
-#pragma unroll
-                for (int e = 0; e < N; ++e) o[0][e] = fmaf(w[e], sc[e], b[e] * sd[e]);
-                vector(a.pre_w, c, 1.f, w);
-                vector(a.pre_b, c, 0.f, b);
+                float pw[N], pb[N], w[N], b[N], gt[N], s1p[N], o[3][N];
+                load_or<N>((const T *)a.post_w, c, 1.f, pw);
+                load_or<N>((const T *)a.post_b, c, 0.f, pb);
+                load_or<N>((const T *)a.pre_w, c, 1.f, w);
+                load_or<N>((const T *)a.pre_b, c, 0.f, b);
+                if (vecs) {
+                    load_or<N>((const T *)a.gate, mod + c, 1.f, gt);
+                    load_or<N>((const T *)a.scale, mod + c, 0.f, s1p);
+                }
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
+                    o[0][e] = fmaf(pw[e], sc[e], pb[e] * sd[e]);
                     o[1][e] = fmaf(w[e], sa[e], b[e] * sb[e]);
                     o[2][e] = sb[e];
                 }
@@ -463,26 +481,27 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
 #pragma unroll
                     for (int e = 0; e < N; e += 4) *reinterpret_cast<f32x4 *>(to + e) = *reinterpret_cast<f32x4 *>(&o[k][e]);
                 }
+                if (!vecs) return;
                 // the norms' vectors: w_post, b_post, w, b
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (g.out[3 + k] == nullptr) continue;
-                    if (k == 0) vector(a.gate, mod + c, 1.f, m);
-                    if (k == 1) vector(a.gate, mod + c, 1.f, m);
-                    if (k >= 2) {
-                        vector(a.scale, mod + c, 0.f, m);
+                for (int e = 0; e < N; ++e) s1p[e] += 1.f;
+                if constexpr (ALONE) {
 #pragma unroll
-                        for (int e = 0; e < N; ++e) m[e] += 1.f;
-                    }
-                    const float *const of = k == 0 ? sc : k == 1 ? sd : k == 2 ? sa : sb;
-                    if constexpr (ALONE) {
+                    for (int i = 0; i < CH; ++i)
+                        if (r.at(i) == c) {
 #pragma unroll
-                        for (int i = 0; i < CH; ++i)
-                            if (r.at(i) == c) {
-#pragma unroll
-                                for (int e = 0; e < N; ++e) vec[k][i][e] = fmaf(m[e], of[e], vec[k][i][e]);
+                            for (int e = 0; e < N; ++e) {
+                                vec[0][i][e] = fmaf(gt[e], sc[e], vec[0][i][e]);
+                                vec[1][i][e] = fmaf(gt[e], sd[e], vec[1][i][e]);
+                                vec[2][i][e] = fmaf(s1p[e], sa[e], vec[2][i][e]);
+                                vec[3][i][e] = fmaf(s1p[e], sb[e], vec[3][i][e]);
                             }
-                    } else {
+                        }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (g.out[3 + k] == nullptr) continue;
+                        const float *const m = k < 2 ? gt : s1p, *const of = k == 0 ? sc : k == 1 ? sd : k == 2 ? sa : sb;
                         float *const to = g.sums + ((long)k * gridDim.x + blockIdx.x) * a.C + c;
 #pragma unroll
                         for (int e = 0; e < N; e += 4) {

@@ -41,10 +41,11 @@ inline NormTeam grad_team(int rows, int C) {
     return {256, c <= 512 ? 2 : c <= 1024 ? 4 : 0};
 }
 
-// Most blocks of a gradient call (512: 230400 x 320 210 us and 30000 x 1536 127
-// against 224 and 136 with 1024, whose partial sums weigh more; 256: 205 and
-// 124, but 71 against 56 at 230400 x 64).
-constexpr int GRAD_BLOCKS = 512;
+// Most blocks of a gradient call: those that run at once, two on a unit, or one
+// where three or four chunks take its registers (another round would pay again
+// for a block's products and sums: 8192 x 1152 45 us by 512 blocks, 41 by 256).
+constexpr int GRAD_BLOCKS = 2 * NORM_CUS;
+inline int grad_most_blocks(NormTeam t) { return t.chunks > 2 ? NORM_CUS : GRAD_BLOCKS; }
 
 // Item i of n_items: rows [start, start + part) of modulation row i / per_group,
 // part i % per_group of it.  alone: a team takes an item by itself, else the
@@ -77,11 +78,11 @@ inline GradPlan grad_plan(int rows, int C, int rows_per_mod, bool mods, bool vec
         g.alone = teams > 1 && per < std::max(2 * teams, 16);
         // (an item's sums cost its share of LDS and of the join: four rows a team where that leaves no unit idle)
         const int least = std::min(std::max(rows / (NORM_CUS * teams), 1), 4) * teams;
-        g.per_group = g.alone ? 1 : std::min(std::max(1, GRAD_BLOCKS / n_mod), div(per, least));
+        g.per_group = g.alone ? 1 : std::min(std::max(1, grad_most_blocks(g.team) / n_mod), div(per, least));
         g.part = div(per, g.per_group);
         g.per_group = div(per, g.part);
         g.n_items = n_mod * g.per_group;
-        g.blocks = std::min(g.alone ? div(g.n_items, teams) : g.n_items, GRAD_BLOCKS);
+        g.blocks = std::min(g.alone ? div(g.n_items, teams) : g.n_items, grad_most_blocks(g.team));
         g.slots = mods && g.per_group > 1 ? up(3 * (size_t)g.n_items * C * 4) : 0;
     }
     g.sums = vecs ? up(4 * (size_t)g.blocks * C * 4) : 0;

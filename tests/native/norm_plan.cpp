@@ -47,7 +47,7 @@ static int check(int rows, int C, int per, bool mods, bool vecs) {
     if (mods && (g.team.chunks == 0 || g.per_group > 1) && g.slots < slot) return bad("slots");
     if (vecs && g.sums < 4 * (size_t)g.blocks * C * 4) return bad("sums");
     if (g.team.chunks == 0 && (g.stats < (size_t)rows * GRAD_ROW_STATS || g.blocks != g.n_items)) return bad("stats");
-    if (T > 1 && g.alone && (long)g.blocks * T < std::min<long>(g.n_items, (long)GRAD_BLOCKS * T)) return bad("teams");
+    if (T > 1 && g.alone && (long)g.blocks * T < std::min<long>(g.n_items, (long)grad_most_blocks(g.team) * T)) return bad("teams");
     // the size that callers are told covers every choice of gradients
     oc_shape sh;
     std::memset(&sh, 0, sizeof(sh));
