@@ -117,6 +117,22 @@ struct Team {
     }
 };
 
+// A row of 8 elements per chunk, kept as it was read.
+template <typename T> struct Raw8 { uint4 v[sizeof(T) / 2]; };
+__device__ __forceinline__ void widen(const Raw8<uint16_t> &r, float (&v)[8]) {
+    const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void widen(const Raw8<float> &r, float (&v)[8]) {
+    const uint32_t w[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+}
+
 template <typename T, int TPR, int CH>
 struct RegRow {
     typedef float Vals[CH][8];
@@ -124,6 +140,19 @@ struct RegRow {
     __device__ __forceinline__ explicit RegRow(int channels) : C(channels), c0(Team<TPR>::lane() * 8) {}
     __device__ __forceinline__ int at(int i) const { return c0 + i * TPR * 8; }
     __device__ __forceinline__ bool in(int i) const { return at(i) < C; }
+    // as it is read (widened where it is used; channels past C: 0)
+    typedef Raw8<T> Raws[CH];
+    __device__ __forceinline__ void fetch(const T *p, Raws &raw) const {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            raw[i] = Raw8<T>{};
+            if (p != nullptr && in(i)) {
+#pragma unroll
+                for (int k = 0; k < (int)sizeof(T) / 2; ++k)
+                    raw[i].v[k] = reinterpret_cast<const uint4 *>(p + at(i))[k];
+            }
+        }
+    }
     // channels past C: other
     __device__ __forceinline__ void load(const T *p, Vals &v, float other) const {
 #pragma unroll
@@ -179,10 +208,26 @@ __global__ __launch_bounds__(256) void k_norm_gate(NormArgs a, T *h, T *n) {
     if (row >= a.rows) return;
     const Row r(a.C);
     const long at = row * a.C, mod = row / a.rows_per_mod * a.ld;
+    // All on their way before the first sum (30000 x 1536: 69 us, 95 with each vector read where it is
+    // used); but three chunks of fp32 would leave two waves to a SIMD (230400 x 320: 227 against 217).
+    constexpr bool EARLY = sizeof(T) == 2 || CH <= 2;
+    typename Row::Raws rx, ry, rg, rs, rt;
+    r.fetch((const T *)a.x + at, rx);
+    r.fetch(a.y != nullptr ? (const T *)a.y + at : nullptr, ry);
+    auto vectors = [&]() {
+        r.fetch(a.scale != nullptr ? (const T *)a.scale + mod : nullptr, rs);
+        r.fetch(a.shift != nullptr ? (const T *)a.shift + mod : nullptr, rt);
+    };
+    if constexpr (EARLY) {
+        r.fetch(a.gate != nullptr ? (const T *)a.gate + mod : nullptr, rg);
+        vectors();
+    }
     typename Row::Vals v, z, w, b;
-    r.load((const T *)a.x + at, v, 0.f);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) widen(rx[i], v[i]);
     if (a.y != nullptr) {
-        r.load((const T *)a.y + at, z, 0.f);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) widen(ry[i], z[i]);
         r.normalise(a.post, a.post_eps, z, red);
         if (a.post_w != nullptr || a.post_b != nullptr) {
             r.load((const T *)a.post_w, w, 1.f);
@@ -192,11 +237,14 @@ __global__ __launch_bounds__(256) void k_norm_gate(NormArgs a, T *h, T *n) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) z[i][e] = r.in(i) ? fmaf(z[i][e], w[i][e], b[i][e]) : 0.f;
         }
-        r.load(a.gate != nullptr ? (const T *)a.gate + mod : nullptr, w, 1.f);
+        if constexpr (!EARLY) r.fetch(a.gate != nullptr ? (const T *)a.gate + mod : nullptr, rg);
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+        for (int i = 0; i < CH; ++i) {
+            float g[8];
+            widen(rg[i], g);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = fmaf(w[i][e], z[i][e], a.res_scale * v[i][e]);
+            for (int e = 0; e < 8; ++e) v[i][e] = fmaf(a.gate != nullptr ? g[e] : 1.f, z[i][e], a.res_scale * v[i][e]);
+        }
         if (h != nullptr) r.store(h + at, v);
     }
     if (n == nullptr) return;
@@ -209,18 +257,21 @@ __global__ __launch_bounds__(256) void k_norm_gate(NormArgs a, T *h, T *n) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e], w[i][e], b[i][e]);
     }
-    if (a.scale != nullptr || a.shift != nullptr) {
-        r.load(a.scale != nullptr ? (const T *)a.scale + mod : nullptr, w, 0.f);
-        r.load(a.shift != nullptr ? (const T *)a.shift + mod : nullptr, b, 0.f);
+    if constexpr (!EARLY) vectors();
+    // (scale and shift that are NULL are zeros)
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+    for (int i = 0; i < CH; ++i) {
+        float s[8], t[8];
+        widen(rs[i], s);
+        widen(rt[i], t);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e], 1.f + w[i][e], b[i][e]);
+        for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e], 1.f + s[e], t[e]);
     }
     r.store(n + at, v);
 }
 
 enum { Q_GATE, Q_SCALE, Q_SHIFT, Q_POSTW, Q_POSTB, Q_PREW, Q_PREB, N_Q };
+
 // Work of the gradients: item i is rows of one modulation row, group
 // i / per_group, split into per_group items.
 struct GradItems {
@@ -229,22 +280,6 @@ struct GradItems {
     float *sums;            // [4][blocks][C]
     int part, per_group, n_items;   // rows of an item
 };
-
-// A row of 8 elements per chunk, kept as it was read.
-template <typename T> struct Raw8 { uint4 v[sizeof(T) / 2]; };
-__device__ __forceinline__ void widen(const Raw8<uint16_t> &r, float (&v)[8]) {
-    const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-}
-__device__ __forceinline__ void widen(const Raw8<float> &r, float (&v)[8]) {
-    const uint32_t w[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-}
 
 // The gradients of rows in registers.  What a row needs of the vectors of its
 // modulation row are three products,
