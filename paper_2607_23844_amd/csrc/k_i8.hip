@@ -7,6 +7,7 @@
 #include "oc_launch.h"
 #include "oc_ops.h"
 #include "oc_ring_tile.h"
+#include <algorithm>
 
 namespace oc {
 
@@ -215,33 +216,63 @@ __device__ __forceinline__ long out_row(const LinearI8Args &a, long r) {
 // bf16 tiles are staged through LDS and written in 16-byte chunks of whole
 // rows, fp32 tiles wave by wave.
 // ---------------------------------------------------------------------------
+// LDS behind the staged rows: scales and biases of the outputs, scales and places
+// of the rows
+template <typename R>
+constexpr size_t LIN_STAGE = std::max<size_t>((size_t)R::BB * (R::BA + 8) * 2, R::NW * 32 * 36 * 4);
+template <typename R>
+constexpr size_t LIN_LDS = std::max<size_t>(R::LDS_BYTES, LIN_STAGE<R> + (R::BA + R::BB) * 8);
+
 template <int ID, typename T, bool GELU>
 __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, int n_at, int n_bt) {
     using R = typename RingShape<ID, RING_I8>::Tile;
     constexpr int BA = R::BA, BB = R::BB;
+    static_assert(BA <= R::NT && BB <= R::NT && LIN_LDS<R> <= 160 * 1024, "a thread for each row and output; LDS");
     extern __shared__ __align__(16) uint16_t lds[];
     int at, bt;
     tile_order(xcd_remap(blockIdx.x, n_at * n_bt), n_at, n_bt, at, bt);
     const int a0 = at * BA, b0 = bt * BB;
     const int K2 = (a.K + 15) / 16 * 8;   // pairs of elements in a row
+    // what the epilogue needs of one output and one row, loaded ahead of the operands
+    const int mine_a = min(a0 + (int)threadIdx.x, a.N - 1), mine_b = min(b0 + (int)threadIdx.x, a.rows - 1);
+    float my_sw = 0.f, my_bias = 0.f, my_sq = 0.f;
+    int my_out = 0;
+    if ((int)threadIdx.x < BA) {
+        my_sw = a.sw[mine_a];
+        if (a.bias != nullptr) my_bias = Elem<T>::ld((const T *)a.bias + mine_a);
+    }
+    if ((int)threadIdx.x < BB) {
+        my_sq = a.sq[mine_b];
+        my_out = a.out_idx != nullptr ? a.out_idx[mine_b] : mine_b;
+    }
     typename R::RowsA ra;
     typename R::RowsB rb;
     ring_rows(ra, (const uint16_t *)a.w, a.N, K2, a0);
     ring_rows(rb, (const uint16_t *)a.q, a.rows, K2, b0);
     R t;
     t.run(lds, ra, rb, K2);
+    float *const col_sw = reinterpret_cast<float *>(reinterpret_cast<char *>(lds) + LIN_STAGE<R>), *const col_b = col_sw + BA;
+    float *const row_sq = col_b + BA;
+    int *const row_out = reinterpret_cast<int *>(row_sq + BB);   // y row, or -1
+    if ((int)threadIdx.x < BA) {
+        col_sw[threadIdx.x] = my_sw;
+        col_b[threadIdx.x] = my_bias;
+    }
+    if ((int)threadIdx.x < BB) {
+        row_sq[threadIdx.x] = my_sq;
+        row_out[threadIdx.x] = b0 + (int)threadIdx.x < a.rows && my_out >= 0 && my_out < a.n_out ? my_out : -1;
+    }
+    __syncthreads();
     float sq[R::TB];
 #pragma unroll
-    for (int j = 0; j < R::TB; ++j) sq[j] = a.sq[min(b0 + R::b_of(j), a.rows - 1)];
+    for (int j = 0; j < R::TB; ++j) sq[j] = row_sq[R::b_of(j)];
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int i = 0; i < R::TA; ++i)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int n = R::a_of(i, g);
-                if (a0 + n >= a.N) continue;
-                f32x4 sw, bias;
-                columns4<T>(a, a0 + n, sw, bias);
+                const f32x4 sw = *reinterpret_cast<const f32x4 *>(col_sw + n), bias = *reinterpret_cast<const f32x4 *>(col_b + n);
 #pragma unroll
                 for (int j = 0; j < R::TB; ++j)
                     *reinterpret_cast<u16x4 *>(lds + R::b_of(j) * (BA + 8) + n) =
@@ -249,7 +280,7 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, 
             }
         __syncthreads();
         write_rows<BA, BB, R::NT>(lds, min(BA, a.N - a0), [&](int b, int c0) -> uint16_t * {
-            const long o = out_row(a, b0 + b);
+            const int o = row_out[b];
             return o >= 0 ? (uint16_t *)a.y + o * a.ld_y + a0 + c0 : nullptr;
         });
     } else {
@@ -258,25 +289,25 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, 
         constexpr int LD = 36;
         const int lane = threadIdx.x & 63;
         float *const mine = reinterpret_cast<float *>(lds) + (threadIdx.x >> 6) * 32 * LD;
-        static_assert(R::NW * 32 * LD * 4 <= R::LDS_BYTES, "the waves' parts fit in the ring");
+        static_assert(LIN_STAGE<R> >= R::NW * 32 * LD * 4, "the waves' parts");
 #pragma unroll
         for (int i = 0; i < R::TA; ++i) {
-            f32x4 sw[4], bias[4];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) columns4<T>(a, min(a0 + R::a_of(i, g), a.N - 4), sw[g], bias[g]);
             const int n = a0 + (R::a_of(i, 0) & ~31) + (lane & 7) * 4;   // outputs that this lane stores
 #pragma unroll
             for (int j = 0; j < R::TB; ++j) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
+                for (int g = 0; g < 4; ++g) {
+                    const int c = R::a_of(i, g);
                     *reinterpret_cast<f32x4 *>(mine + (lane & 31) * LD + 8 * g + 4 * (lane >> 5)) =
-                        finish4<GELU>(four(t.acc[i][j], g), sq[j], sw[g], bias[g]);
+                        finish4<GELU>(four(t.acc[i][j], g), sq[j], *reinterpret_cast<const f32x4 *>(col_sw + c),
+                                      *reinterpret_cast<const f32x4 *>(col_b + c));
+                }
                 wave_lds_fence();
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int r = k * 8 + (lane >> 3);
                     const f32x4 v = *reinterpret_cast<const f32x4 *>(mine + r * LD + (lane & 7) * 4);
-                    const long o = out_row(a, b0 + (R::b_of(j) & ~31) + r);
+                    const int o = row_out[(R::b_of(j) & ~31) + r];
                     if (o >= 0 && n < a.N) *reinterpret_cast<f32x4 *>((T *)a.y + o * a.ld_y + n) = v;
                 }
                 wave_lds_fence();
@@ -361,10 +392,10 @@ hipError_t go_ring(const LinearI8Args &a, hipStream_t st) {
     return ring_dispatch(id, [&](auto c) -> hipError_t {
         constexpr int ID = decltype(c)::value;
         using R = typename RingShape<ID, RING_I8>::Tile;
-        const hipError_t e = allow_lds(k_linear_i8<ID, T, GELU>, R::LDS_BYTES);
+        const hipError_t e = allow_lds(k_linear_i8<ID, T, GELU>, LIN_LDS<R>);
         if (e != hipSuccess) return e;
         const int n_at = cdiv(a.N, R::BA), n_bt = cdiv(a.rows, R::BB);
-        launch_k(k_linear_i8<ID, T, GELU>, (unsigned)(n_at * n_bt), R::NT, R::LDS_BYTES, st, a, n_at, n_bt);
+        launch_k(k_linear_i8<ID, T, GELU>, (unsigned)(n_at * n_bt), R::NT, LIN_LDS<R>, st, a, n_at, n_bt);
         return hipGetLastError();
     });
 }
