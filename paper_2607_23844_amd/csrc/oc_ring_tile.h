@@ -360,8 +360,9 @@ inline float ring_cost(const RingShapeCost &c, int nk, long blocks, float epi = 
 // The shape with the lowest cost for K elements; tiles(BA, BB): tiles of the
 // launch.  Not more threads than a grid holds (the narrow shapes, on half a
 // billion rows of few columns); room for the blocks that convert weights.
+// costs: the shapes in the same order with figures of another kernel.
 template <typename Tiles>
-inline int ring_pick(int K, Tiles tiles) {
+inline int ring_pick(int K, Tiles tiles, const RingShapeCost (&costs)[N_RING_SHAPES] = RING_SHAPES) {
     constexpr int threads[N_RING_SHAPES] = {RING_THREADS<0>, RING_THREADS<1>, RING_THREADS<2>, RING_THREADS<3>,
                                             RING_THREADS<4>, RING_THREADS<5>, RING_THREADS<6>, RING_THREADS<7>,
                                             RING_THREADS<8>, RING_THREADS<9>};
@@ -369,9 +370,9 @@ inline int ring_pick(int K, Tiles tiles) {
     int best = 0;
     float best_t = 0.f;
     for (int i = 0; i < N_RING_SHAPES; ++i) {
-        const long n = tiles(RING_SHAPES[i].BA, RING_SHAPES[i].BB);
+        const long n = tiles(costs[i].BA, costs[i].BB);
         if (i > 0 && (n + 1024) * threads[i] >= MAX_GRID_THREADS) continue;
-        const float t = ring_cost(RING_SHAPES[i], nk, n);
+        const float t = ring_cost(costs[i], nk, n);
         if (i == 0 || t < best_t) {
             best = i;
             best_t = t;
