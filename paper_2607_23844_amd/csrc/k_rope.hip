@@ -20,41 +20,29 @@ namespace oc {
 namespace {
 
 template <typename T, int V> struct Chunk { typedef T type __attribute__((ext_vector_type(V))); };
-template <typename T> struct Chunk<T, 1> { typedef T type; };
 
 template <typename T, int V>
 __device__ __forceinline__ void get(const T *p, float (&v)[V]) {
     typedef typename Chunk<T, V>::type C;
     const C c = *reinterpret_cast<const C *>(p);
-    if constexpr (V == 1) v[0] = (float)c;
-    else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (float)c[i];
-    }
+    for (int i = 0; i < V; ++i) v[i] = (float)c[i];
 }
 template <typename T, int V>
 __device__ __forceinline__ void put(T *p, const float (&v)[V]) {
     typedef typename Chunk<T, V>::type C;
     C c;
-    if constexpr (V == 1) c = (T)v[0];
-    else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) c[i] = (T)v[i];
-    }
+    for (int i = 0; i < V; ++i) c[i] = (T)v[i];
     *reinterpret_cast<C *>(p) = c;
 }
 
 constexpr int ROPE_ROWS = 16;   // most rows of a block
 struct Turn { float c, s; };
 
-// PAIRS: unit u is channels 8u..8u+7 (V = 4 pairs); else channels lo.. and hi.. of V pairs
-template <typename T, bool PAIRS, int V>
-__global__ __launch_bounds__(256) void k_rope(RopeGeom g, RopeArgs a, int block_rows) {
-    __shared__ __align__(16) Turn turns[ROPE_ROWS * ROPE_MAX_PAIRS];
-    __shared__ int where[ROPE_ROWS][4];   // position on the axes; whether there is one
-    const long row0 = (long)folded_block() * block_rows;
-    if (row0 >= a.rows) return;
-    const int rows = (int)min((long)block_rows, a.rows - row0);
+// Positions and turns of a block's rows, by all of its 256 threads.
+__device__ __forceinline__ void make_turns(const RopeGeom &g, const RopeArgs &a, long row0, int rows,
+                                           int (*where)[4], Turn *turns) {
     if ((int)threadIdx.x < rows) {
         const long row = row0 + threadIdx.x;
         int *const w = where[threadIdx.x];
@@ -81,6 +69,17 @@ __global__ __launch_bounds__(256) void k_rope(RopeGeom g, RopeArgs a, int block_
         turns[r * ROPE_MAX_PAIRS + p] = Turn{cospif(x), a.inverse ? -sn : sn};
     }
     __syncthreads();
+}
+
+// PAIRS: unit u is channels 8u..8u+7 (V = 4 pairs); else channels lo.. and hi.. of V pairs
+template <typename T, bool PAIRS, int V>
+__global__ __launch_bounds__(256) void k_rope(RopeGeom g, RopeArgs a, int block_rows) {
+    __shared__ __align__(16) Turn turns[ROPE_ROWS * ROPE_MAX_PAIRS];
+    __shared__ int where[ROPE_ROWS][4];   // position on the axes; whether there is one
+    const long row0 = (long)folded_block() * block_rows;
+    if (row0 >= a.rows) return;
+    const int rows = (int)min((long)block_rows, a.rows - row0);
+    make_turns(g, a, row0, rows, where, turns);
     const int units = g.dh / 2 / V, q_units = a.q != nullptr ? a.heads * units : 0;
     const int row_units = q_units + (a.k != nullptr ? a.k_heads * units : 0);
     constexpr int N = 4, W = PAIRS ? 8 : V;   // units at a time; channels of a run
@@ -137,24 +136,76 @@ __global__ __launch_bounds__(256) void k_rope(RopeGeom g, RopeArgs a, int block_
     }
 }
 
-template <typename T, bool PAIRS, int V>
-hipError_t go_rope(const RopeGeom &g, const RopeArgs &a, hipStream_t st) {
-    // rows of a block: all that leave two blocks for every unit
-    int rows = 1;
-    while (rows < ROPE_ROWS && a.rows / (2 * rows) >= 2 * N_CUS) rows *= 2;
-    launch_k(k_rope<T, PAIRS, V>, folded_grid((a.rows + rows - 1) / rows, 256), 256, 0, st, g, a, rows);
-    return hipGetLastError();
+// Halves whose sections fit no run of four channels: heads pass through LDS,
+// read and written in 16-byte chunks, and a wave turns a head there, one pair
+// per lane (access by single channels took 39 us for 4096 rows of 2 x 12 heads
+// of 128).
+constexpr int ROPE_LDS = 8192;   // channels at a time
+template <typename T>
+__global__ __launch_bounds__(256) void k_rope_lds(RopeGeom g, RopeArgs a, int block_rows) {
+    __shared__ __align__(16) Turn turns[ROPE_ROWS * ROPE_MAX_PAIRS];
+    __shared__ int where[ROPE_ROWS][4];
+    __shared__ __align__(16) T data[ROPE_LDS];
+    const long row0 = (long)folded_block() * block_rows;
+    if (row0 >= a.rows) return;
+    const int rows = (int)min((long)block_rows, a.rows - row0);
+    make_turns(g, a, row0, rows, where, turns);
+    const int q_heads = a.q != nullptr ? a.heads : 0, heads = q_heads + (a.k != nullptr ? a.k_heads : 0);
+    const int total = rows * heads, most = ROPE_LDS / g.dh, cpr = g.dh / 8;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int lo = 0, hi = 0;   // this lane's pair
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+        if (lane >= g.sect[m] && lane < g.sect[m + 1]) {
+            lo = g.sect[m] + lane;
+            hi = lo + g.sect[m + 1] - g.sect[m];
+        }
+    // chunk c of heads h0, h0 + 1, ... of the block's rows (nullptr: a row without a position)
+    auto chunk = [&](int h0, int c, const void *q, const void *k, long ld_q, long ld_k) -> T * {
+        const int s = h0 + c / cpr, r = s / heads;
+        int h = s - r * heads;
+        if (!where[r][3]) return nullptr;
+        const bool is_k = h >= q_heads;
+        if (is_k) h -= q_heads;
+        return (T *)(is_k ? k : q) + (row0 + r) * (is_k ? ld_k : ld_q) + h * g.dh + (c % cpr) * 8;
+    };
+    typedef typename Chunk<T, 8>::type C8;
+    for (int h0 = 0; h0 < total; h0 += most) {
+        const int n = min(most, total - h0);
+        for (int c = threadIdx.x; c < n * cpr; c += 256) {
+            const T *p = chunk(h0, c, a.q, a.k, a.ld_q, a.ld_k);
+            if (p != nullptr) *reinterpret_cast<C8 *>(data + c * 8) = *reinterpret_cast<const C8 *>(p);
+        }
+        __syncthreads();
+        if (lane < g.P) {
+            for (int s = wave; s < n; s += 4) {
+                const Turn t = turns[(h0 + s) / heads * ROPE_MAX_PAIRS + lane];
+                T &x = data[s * g.dh + lo], &y = data[s * g.dh + hi];
+                const float x0 = (float)x, y0 = (float)y;
+                x = (T)fmaf(x0, t.c, -(y0 * t.s));
+                y = (T)fmaf(x0, t.s, y0 * t.c);
+            }
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < n * cpr; c += 256) {
+            T *p = chunk(h0, c, a.qo, a.ko, a.ld_qo, a.ld_ko);
+            if (p != nullptr) *reinterpret_cast<C8 *>(p) = *reinterpret_cast<const C8 *>(data + c * 8);
+        }
+        __syncthreads();
+    }
 }
 
 template <typename T>
 hipError_t type_rope(const RopeGeom &g, const RopeArgs &a, hipStream_t st) {
-    if (g.pairs) return go_rope<T, true, 4>(g, a, st);
-    switch (g.vec) {
-        case 8: return go_rope<T, false, 8>(g, a, st);
-        case 4: return go_rope<T, false, 4>(g, a, st);
-        case 2: return go_rope<T, false, 2>(g, a, st);
-        default: return go_rope<T, false, 1>(g, a, st);
-    }
+    // rows of a block: all that leave two blocks for every unit
+    int rows = 1;
+    while (rows < ROPE_ROWS && a.rows / (2 * rows) >= 2 * N_CUS) rows *= 2;
+    auto go = [&](auto kern) {
+        launch_k(kern, folded_grid((a.rows + rows - 1) / rows, 256), 256, 0, st, g, a, rows);
+        return hipGetLastError();
+    };
+    if (g.pairs) return go(k_rope<T, true, 4>);
+    return g.vec == 8 ? go(k_rope<T, false, 8>) : g.vec == 4 ? go(k_rope<T, false, 4>) : go(k_rope_lds<T>);
 }
 
 }  // namespace

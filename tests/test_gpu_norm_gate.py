@@ -202,6 +202,9 @@ def test_zero_rows_and_zero_deviation():
     w = torch.ones(64, device=DEV)
     h, n = oc.norm_gate(x, sh, y=x, pre=oc.Norm("rms", 1e-6, w))
     assert h.shape == n.shape == (0, 64)
+    # sums over no rows are zero
+    out = oc.norm_gate_grad(x, sh, dn=x, y=x, pre=oc.Norm("rms", 1e-6, w), post=oc.Norm("layer", 1e-6, w, w))
+    assert out["dx"].shape == (0, 64) and all((out[k] == 0).all() for k in ("pre_w", "post_w", "post_b"))
     # a row without deviation: eps keeps it finite
     c = torch.full((2, 64), 3.0, device=DEV)
     assert torch.equal(oc.norm_gate(c, sh, pre=oc.Norm("layer", 1e-6))[1], torch.zeros_like(c))

@@ -74,10 +74,12 @@ def test_given_positions_far_and_negative(layout, dtype):
     assert torch.equal(qo[0], q[0])
 
 
-@pytest.mark.parametrize("layout", ["pairs", "halves"])
-def test_columns_of_a_projected_buffer_and_in_place(layout):
+ODD = oc.Rope((22, 26, 22), layout="halves")      # halves of 11, 13 and 11: no run of four channels
+
+
+@pytest.mark.parametrize("rp", [oc.Rope((24, 24, 24)), oc.Rope((24, 24, 24), layout="halves"), ODD])
+def test_columns_of_a_projected_buffer_and_in_place(rp):
     sh = oc.Shape(**GRID, C=4 * 72, heads=4, head_dim=72)
-    rp = oc.Rope((24, 24, 24), layout=layout)
     buf = make(5, 180, 6 * 72 + 8, dtype=torch.bfloat16)
     q, k = buf[:, :4 * 72].unflatten(1, (4, 72)), buf[:, 4 * 72:5 * 72].unflatten(1, (1, 72))
     qo, ko = oc.rope_qk(q, k, rp, sh)
@@ -92,10 +94,10 @@ def test_columns_of_a_projected_buffer_and_in_place(layout):
     assert torch.equal(out[:, :4 * 72], torch.zeros_like(out[:, :4 * 72])) and out[:, 4 * 72:5 * 72].any()
 
 
-def test_rows_without_a_token_are_left_alone():
-    sh = oc.Shape(**GRID, C=128, heads=2, head_dim=64)
-    rp = oc.Rope((16, 24, 24))
-    q, k = make(1, 5, 2, 64, dtype=torch.bfloat16), make(2, 5, 2, 64, dtype=torch.bfloat16)
+@pytest.mark.parametrize("rp", [oc.Rope((16, 24, 24)), ODD])
+def test_rows_without_a_token_are_left_alone(rp):
+    sh = oc.Shape(**GRID, C=144, heads=2, head_dim=72)
+    q, k = make(1, 5, 2, 72, dtype=torch.bfloat16), make(2, 5, 2, 72, dtype=torch.bfloat16)
     idx = torch.tensor([179, -1, 180, 3, -(1 << 31)], dtype=torch.int32, device=DEV)
     qo, ko = torch.full_like(q, 7.0), torch.full_like(k, 7.0)
     oc.rope_qk(q, k, rp, sh, kept_idx=idx, q_out=qo, k_out=ko)
@@ -116,6 +118,20 @@ def test_not_finite_values_stay_in_their_pair():
     bad[71, 0, 63] = True
     assert torch.equal(out[~bad], ref[~bad])
     assert out[71, 0, 63] == float("-inf") and out[70, 0, 40].isnan()
+
+
+@pytest.mark.parametrize("rp", [oc.Rope((48, 40, 40)), oc.Rope((48, 40, 40), layout="halves"), ODD])
+def test_many_rows_and_heads(rp):
+    """Blocks of several rows, more heads than one of them holds at a time."""
+    sh = oc.Shape(3, 30, 31, 33 * 128, 33, 128)
+    q, k = make(1, 2790, 33, 128, dtype=torch.bfloat16), make(2, 2790, 7, 128, dtype=torch.bfloat16)
+    idx = torch.randint(-40, 2830, (2790,), generator=torch.Generator().manual_seed(5)).int().to(DEV)
+    qo, ko = oc.rope_qk(q, k, rp, sh, kept_idx=idx, q_out=q.clone(), k_out=k.clone())
+    ok = (idx >= 0) & (idx < 2790)
+    pos = grid_pos(idx[ok], 30, 31)
+    check(qo[ok], *rope(q[ok], pos, rp), N_ROUND, "q")
+    check(ko[ok], *rope(k[ok], pos, rp), N_ROUND, "k")
+    assert torch.equal(qo[~ok], q[~ok]) and torch.equal(ko[~ok], k[~ok])
 
 
 def test_gradient_is_the_transpose():
