@@ -219,9 +219,13 @@ def attn_reduced(x_kept: torch.Tensor, n_seq: int, seq_len: int, weights: Dict[s
     if ws is None:
         ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
     if rope is not None:
+        if kept_idx is None:
+            raise L.OmniCacheError(L.OC_ERR_INVALID_ARG, "rotary positions need the rows' tokens: kept_idx is None")
         _need(kept_idx, torch.int32, "kept_idx")
         if kept_idx.numel() != n_seq * seq_len:
             raise L.OmniCacheError(L.OC_ERR_SHAPE, f"kept_idx has {kept_idx.numel()} entries for {n_seq * seq_len} rows")
+        if kept_idx.device != dev:
+            raise L.OmniCacheError(L.OC_ERR_INVALID_ARG, f"kept_idx is on {kept_idx.device}, expected {dev}")
     sh = shape.c()
     L.check(L.lib().oc_attn_reduced_rope(C.byref(sh), _rope(rope), _ptr(kept_idx), x_kept.data_ptr(), n_seq, seq_len,
                                          _ptr(ctx), C.byref(w), y.data_ptr(), _ptr(y_ctx), ws.data_ptr(), ws.numel(),
