@@ -8,6 +8,7 @@ need not be the current one; the work goes on that GPU's current stream.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from dataclasses import dataclass
 from typing import Dict, Optional, Sequence, Tuple
 
@@ -53,13 +54,18 @@ def _call(name: str, dev: torch.device, *args) -> None:
         L.check(status)
 
 
+@functools.lru_cache(maxsize=256)
+def _made(v):
+    return C.byref(v.c())
+
+
 def _struct(v):
-    """C.byref of the C struct of a Shape or Rope (immutable: made once)."""
-    ref = v.__dict__.get("_ref")
-    if ref is None:
-        ref = C.byref(v.c())
-        object.__setattr__(v, "_ref", ref)
-    return ref
+    """C.byref of the C struct of a Shape or Rope, made once for equal ones (the
+    library only reads it)."""
+    try:
+        return _made(v)
+    except TypeError:      # (a Rope of lists has no hash)
+        return C.byref(v.c())
 
 
 def _gpu(t, name: str) -> torch.Tensor:

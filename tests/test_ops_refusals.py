@@ -305,3 +305,15 @@ def test_i8_rows_and_empty_calls():
 def test_norm_gradient_plan_covers_its_rows_and_workspace(native):
     r = native("norm_plan")()
     assert r.returncode == 0, r.stdout[:2000]
+
+
+def test_calls_leave_shapes_as_they_are():
+    """Shapes and positions stay plain values: they can be pickled after a call
+    that made their C structs, and equal ones share them."""
+    import pickle
+    from paper_2607_23844_amd import ops
+    for v in (oc.Shape(1, 4, 4, 128, 2, 64), oc.Rope((0, 32, 32)), oc.Rope([0, 32, 32])):
+        ops._struct(v)
+        assert pickle.loads(pickle.dumps(v)) == v
+    a, b = oc.Shape(1, 4, 4, 128, 2, 64), oc.Shape(1, 4, 4, 128, 2, 64, dtype="f32")
+    assert ops._struct(a)._obj.dtype == L.OC_BF16 and ops._struct(b)._obj.dtype == L.OC_F32
