@@ -203,16 +203,20 @@ def norm_gate_grad(x: torch.Tensor, shape: Shape, dn: Optional[torch.Tensor] = N
             raise _bad(L.OC_ERR_INVALID_ARG, f"unknown gradients {sorted(set(want) - set(GRADS))}")
         has = [k for k in has if k in want]
     at = dict(out)
-    for k in has:
-        t = out[k] = torch.empty((n_mod, shape.C) if k in ("gate", "scale", "shift") else (shape.C,),
-                                 dtype=torch.float32, device=dev)
-        at[k] = t.data_ptr()
+    # the vectors' gradients: one block for the modulation's, one for the norms'
+    for names, size in (([k for k in has if k in GRADS[2:5]], (n_mod, shape.C)),
+                        ([k for k in has if k in GRADS[5:]], (shape.C,))):
+        if names:
+            block = x.new_empty((len(names), *size), dtype=torch.float32)
+            base, step = block.data_ptr(), block.stride(0) * 4
+            for i, (k, t) in enumerate(zip(names, block.unbind(0))):
+                out[k], at[k] = t, base + i * step
     for k, there in (("dx", True), ("dy", y is not None)):
         if there and (want is None or k in want):
             out[k] = torch.empty_like(x)
             at[k] = out[k].data_ptr()
     if ws is None:
-        ws = torch.empty(max(norm_gate_grad_workspace_bytes(shape, rows, per), 256), dtype=torch.uint8, device=dev)
+        ws = x.new_empty((max(norm_gate_grad_workspace_bytes(shape, rows, per), 256),), dtype=torch.uint8)
     elif _gpu(ws, "ws").device != dev or not ws.is_contiguous():
         raise _bad(L.OC_ERR_INVALID_ARG, f"ws must be contiguous and on {dev}")
     g = L.oc_norm_grads(*(at[k] for k in GRADS[2:]))
@@ -261,12 +265,12 @@ def rope_qk(q: Optional[torch.Tensor], k: Optional[torch.Tensor], rope: Rope, sh
     qp, ldq, _ = _heads_of(q, rows, shape.heads, shape, dev, "q")
     kp, ldk, kh = _heads_of(k, rows, None, shape, dev, "k")
     if q_out is None and q is not None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         qop, ldqo = q_out.data_ptr(), shape.heads * shape.head_dim
     else:
         qop, ldqo, _ = _heads_of(q_out, rows, shape.heads, shape, dev, "q_out")
     if k_out is None and k is not None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
         kop, ldko = k_out.data_ptr(), kh * shape.head_dim
     else:
         kop, ldko, _ = _heads_of(k_out, rows, kh, shape, dev, "k_out")
@@ -304,12 +308,12 @@ def quant_rows(x: torch.Tensor, row_idx: Optional[torch.Tensor] = None, q: Optio
     ip = _ids(row_idx, (rows,), dev, "row_idx")
     Kp = (K + 15) // 16 * 16
     if q is None:
-        q = torch.empty((rows, Kp), dtype=torch.int8, device=dev)
+        q = x.new_empty((rows, Kp), dtype=torch.int8)
         qp = q.data_ptr()
     else:
         qp = _like(q, (rows, Kp), torch.int8, dev, "q")
     if scale is None:
-        scale = torch.empty((rows,), dtype=torch.float32, device=dev)
+        scale = x.new_empty((rows,), dtype=torch.float32)
         sp = scale.data_ptr()
     else:
         sp = _like(scale, (rows,), torch.float32, dev, "scale")
@@ -339,7 +343,7 @@ def linear_i8(q: torch.Tensor, scale: torch.Tensor, w: torch.Tensor, w_scale: to
     if y is None:
         if out_idx is not None:
             raise _bad(L.OC_ERR_INVALID_ARG, "out_idx needs y, the tensor whose rows it names")
-        y = torch.empty((rows, N), dtype=torch.bfloat16 if dtype is None else dtype, device=dev)
+        y = q.new_empty((rows, N), dtype=torch.bfloat16 if dtype is None else dtype)
     at, ld = _matrix(y, "y")
     if y.device != dev or y.shape[1] != N or (dtype is not None and y.dtype != dtype):
         raise _bad(L.OC_ERR_SHAPE, f"y is {tuple(y.shape)} {y.dtype} on {y.device}, expected [..., {N}] on {dev}")
