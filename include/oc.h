@@ -516,7 +516,9 @@ oc_status oc_rope_qk(const oc_shape *shape, const oc_rope *rope, int32_t n_rows,
  * are not turned).  bf16 layers hold q and k in fp16 before and after the
  * rotation (a second rounding of 2^-11); head_dim 64 layers of short
  * sequences give up the fused projection and attention for it.  Workspaces
- * as without _rope.
+ * as without _rope.  (oc_layer_cached_static and oc_block_cached have no such
+ * form: a block with positions is two oc_layer_cached_rope calls and
+ * oc_residual_add or oc_norm_gate between them.)
  */
 oc_status oc_attn_reduced_rope(const oc_shape *shape, const oc_rope *rope, const int32_t *kept_idx,
                                const void *x_kept, int32_t n_seq, int32_t seq_len, const void *ctx,

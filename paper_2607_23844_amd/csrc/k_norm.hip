@@ -301,7 +301,7 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
     typedef RegRow<T, TPR, CH> Row;
     typedef typename Row::Vals Vals;
     constexpr int TEAMS = Team<TPR>::PER_BLOCK, CP = TPR * CH * 8;
-    extern __shared__ __align__(16) float lds[];   // P, Q, R [2][CP / 2] each (not ALONE); [team][CP]
+    extern __shared__ __align__(16) float lds[];   // P, Q, R [2][CP / 2] each (not ALONE); [sum][team][CP]
     float *const comb = lds + (ALONE ? 0 : 3 * CP);
     __shared__ float red[8];
     const Row r(a.C);
@@ -553,31 +553,24 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
                     if (r.in(i)) emit(r.at(i), std::integral_constant<int, 8>{}, sum[0][i], sum[1][i], sum[2][i], sum[3][i]);
             } else {
                 // the teams' sums: this thread's channels, four at a time (CP is a multiple of 128)
-                constexpr int MINE = (CP + 1023) / 1024;
-                f32x4 tot[4][MINE];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
-                    for (int i = 0; i < CH; ++i) store8(comb + team * CP + r.at(i), sum[k][i]);
-                    __syncthreads();
+                    for (int i = 0; i < CH; ++i) store8(comb + (k * TEAMS + team) * CP + r.at(i), sum[k][i]);
+                __syncthreads();
+                for (int c = threadIdx.x * 4; c < a.C; c += 1024) {
+                    f32x4 tot[4];
 #pragma unroll
-                    for (int j = 0; j < MINE; ++j) {
-                        const int c = threadIdx.x * 4 + j * 1024;
-                        if (c >= CP) continue;
-                        f32x4 v = *reinterpret_cast<const f32x4 *>(comb + c);
-#pragma unroll
-                        for (int o = 1; o < TEAMS; ++o) v += *reinterpret_cast<const f32x4 *>(comb + o * CP + c);
-                        tot[k][j] = v;
+                    for (int k = 0; k < 4; ++k) {
+                        tot[k] = *reinterpret_cast<const f32x4 *>(comb + k * TEAMS * CP + c);
+#pragma unroll 3
+                        for (int o = 1; o < TEAMS; ++o)
+                            tot[k] += *reinterpret_cast<const f32x4 *>(comb + (k * TEAMS + o) * CP + c);
                     }
-                    __syncthreads();
+                    emit(c, std::integral_constant<int, 4>{}, (const float *)&tot[0], (const float *)&tot[1],
+                         (const float *)&tot[2], (const float *)&tot[3]);
                 }
-#pragma unroll
-                for (int j = 0; j < MINE; ++j) {
-                    const int c = threadIdx.x * 4 + j * 1024;
-                    if (c < a.C)
-                        emit(c, std::integral_constant<int, 4>{}, (const float *)&tot[0][j], (const float *)&tot[1][j],
-                             (const float *)&tot[2][j], (const float *)&tot[3][j]);
-                }
+                // (the next item's sums are written behind its barriers)
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) clear(sum[k]);
@@ -978,7 +971,7 @@ static hipError_t go_norm_grad(const NormArgs &a, const T *dh, const T *dn, T *d
     constexpr int TEAMS = Team<TPR>::PER_BLOCK, CP = TPR * CH * 8;
     GradItems g{{q.gate, q.scale, q.shift, q.post_w, q.post_b, q.pre_w, q.pre_b}, (float *)ws,
                 (float *)((char *)ws + p.slots), p.part, p.per_group, p.n_items};
-    const size_t lds = ((ALONE ? 0 : 3) + (SUMS && (ALONE || TEAMS > 1) ? TEAMS : 0)) * (size_t)CP * 4;
+    const size_t lds = ((ALONE ? 0 : 3) + (!SUMS || TEAMS == 1 ? 0 : ALONE ? TEAMS : 4 * TEAMS)) * (size_t)CP * 4;
     const hipError_t e = raise_lds_limit((const void *)k_norm_grad<T, TPR, CH, SUMS, ALONE>, lds);
     if (e != hipSuccess) return e;
     launch_k(k_norm_grad<T, TPR, CH, SUMS, ALONE>, p.blocks, 256, lds, st, a, dh, dn, dx, dy, g);
