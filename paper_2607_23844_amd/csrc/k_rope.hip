@@ -1,17 +1,14 @@
 // Rotary positions of q and k rows with up to three axes.
 //
 // A block turns `rows` rows.  First the cosines and sines of its rows' pairs, one
-// per thread, into LDS: a position times turns per position in 64 bits, less
-// the whole turns, then cospi and sinpi of a fp32 fraction of at most a half
-// (positions of 2^20 would lose 2^-4 of a turn in 32 bits).  Then all heads of
-// q and k of those rows, in units of 8 neighbouring channels (pairs side by
+// per thread, into LDS (oc_rope.h).  Then all heads of q and k of those rows, in units of 8 neighbouring channels (pairs side by
 // side) or of V channels and their V partners half a section further;
 // consecutive threads take consecutive units, four of them loaded at a time.
 // Bound by q's and k's way through HBM.
 #include "oc_attn_common.h"
 #include "oc_device.h"
 #include "oc_launch.h"
-#include "oc_ops.h"
+#include "oc_rope.h"
 #include <cmath>
 #include <cstring>
 
@@ -38,7 +35,6 @@ __device__ __forceinline__ void put(T *p, const float (&v)[V]) {
 }
 
 constexpr int ROPE_ROWS = 16;   // most rows of a block
-struct Turn { float c, s; };
 
 // Positions and turns of a block's rows, by all of its 256 threads.
 __device__ __forceinline__ void make_turns(const RopeGeom &g, const RopeArgs &a, long row0, int rows,
@@ -63,10 +59,9 @@ __device__ __forceinline__ void make_turns(const RopeGeom &g, const RopeArgs &a,
     }
     __syncthreads();
     for (int e = threadIdx.x; e < rows * g.P; e += 256) {
-        const int r = e / g.P, p = e - r * g.P, axis = p < g.axis1 ? 0 : p < g.axis2 ? 1 : 2;
-        const double t = ((double)where[r][axis] + g.origin[axis]) * g.turn[p];
-        const float x = 2.f * (float)(t - rint(t)), sn = sinpif(x);
-        turns[r * ROPE_MAX_PAIRS + p] = Turn{cospif(x), a.inverse ? -sn : sn};
+        const int r = e / g.P, p = e - r * g.P, axis = rope_axis(g, p);
+        const Turn t = rope_turn(rope_fraction(where[r][axis], g.origin[axis], g.turn[p]));
+        turns[r * ROPE_MAX_PAIRS + p] = Turn{t.c, a.inverse ? -t.s : t.s};
     }
     __syncthreads();
 }
@@ -125,10 +120,7 @@ __global__ __launch_bounds__(256) void k_rope(RopeGeom g, RopeArgs a, int block_
             for (int j = 0; j < V; ++j) {
                 if (first[b] + j >= g.P) break;   // (not turned)
                 const Turn t = turns[of[b] + first[b] + j];
-                float &x = PAIRS ? v[b][2 * j] : v[b][j], &y = PAIRS ? v[b][2 * j + 1] : w[PAIRS ? 0 : b][j];
-                const float x0 = x, y0 = y;
-                x = fmaf(x0, t.c, -(y0 * t.s));
-                y = fmaf(x0, t.s, y0 * t.c);
+                turn_pair(PAIRS ? v[b][2 * j] : v[b][j], PAIRS ? v[b][2 * j + 1] : w[PAIRS ? 0 : b][j], t);
             }
             put<T, W>(to[b], v[b]);
             if constexpr (!PAIRS) put<T, W>(to[b] + gap[b], w[b]);
@@ -153,13 +145,8 @@ __global__ __launch_bounds__(256) void k_rope_lds(RopeGeom g, RopeArgs a, int bl
     const int q_heads = a.q != nullptr ? a.heads : 0, heads = q_heads + (a.k != nullptr ? a.k_heads : 0);
     const int total = rows * heads, most = ROPE_LDS / g.dh, cpr = g.dh / 8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int lo = 0, hi = 0;   // this lane's pair
-#pragma unroll
-    for (int m = 0; m < 4; ++m)
-        if (lane >= g.sect[m] && lane < g.sect[m + 1]) {
-            lo = g.sect[m] + lane;
-            hi = lo + g.sect[m + 1] - g.sect[m];
-        }
+    int lo, hi;   // this lane's pair
+    rope_channels(g, lane, lo, hi);
     // chunk c of heads h0, h0 + 1, ... of the block's rows (nullptr: a row without a position)
     auto chunk = [&](int h0, int c, const void *q, const void *k, long ld_q, long ld_k) -> T * {
         const int s = h0 + c / cpr, r = s / heads;
@@ -181,9 +168,10 @@ __global__ __launch_bounds__(256) void k_rope_lds(RopeGeom g, RopeArgs a, int bl
             for (int s = wave; s < n; s += 4) {
                 const Turn t = turns[(h0 + s) / heads * ROPE_MAX_PAIRS + lane];
                 T &x = data[s * g.dh + lo], &y = data[s * g.dh + hi];
-                const float x0 = (float)x, y0 = (float)y;
-                x = (T)fmaf(x0, t.c, -(y0 * t.s));
-                y = (T)fmaf(x0, t.s, y0 * t.c);
+                float u = (float)x, v = (float)y;
+                turn_pair(u, v, t);
+                x = (T)u;
+                y = (T)v;
             }
         }
         __syncthreads();

@@ -12,7 +12,7 @@
 // fp32 accumulation; Q scaled by log2(e)/sqrt(dh)).  The epilogue stages Q
 // and K by slot rows and V transposed (d rows, slot positions permuted inside
 // 16-slot blocks as the Vt layout of the long-sequence kernels), all fp16 in
-// LDS.  Each wave then takes 32 query slots: S^T = K Q^T over the 32-slot key
+// LDS, where a layer with rotary positions turns them.  Each wave then takes 32 query slots: S^T = K Q^T over the 32-slot key
 // blocks that hold its queries' sequences, keys of other sequences masked,
 // the exact maximum, P = exp2(s - max) in fp16, the running sum of that
 // fp16 P, O^T = Vt P^T, and O = O^T / sum written by rows [rows, H*dh].
@@ -22,6 +22,7 @@
 #include "oc_mfma_tile.h"
 #include "oc_ring_tile.h"
 #include "oc_attn_common.h"
+#include "oc_rope.h"
 
 namespace oc {
 
@@ -34,15 +35,81 @@ constexpr int SH_DH = 64;
 constexpr int QKS = 128 + 8;   // LDS row of a slot: Q (64) | K (64) | pad, halves
 constexpr int VTS = 128 + 8;   // LDS row of one V dim over the 128 slots, halves
 constexpr size_t SH_STAGE_BYTES = (size_t)(128 * QKS + SH_DH * VTS) * 2;
-static_assert(SH_STAGE_BYTES <= ShortTile::LDS_BYTES, "staging fits in the ring");
+static_assert(SH_STAGE_BYTES % 16 == 0 && SH_STAGE_BYTES + 128 * 16 <= ShortTile::LDS_BYTES, "staging fits in the ring");
 }  // namespace
 
+// The rotation of Q and K (ROPE) and its row -> token table, if not rm's.
+struct NoRope {};
+struct ShortRope {
+    RopeGeom g;
+    const int *idx;
+};
+
+// Turns the staged Q and K of the block's slots in place: a thread takes V pairs
+// of a slot's Q and K, so an angle is made once for the two, and their channels
+// in runs.  A cached layer of 25 x 72 x 128 tokens, 5 heads: 320 us without the
+// rotation, 336 with one axis of pairs, 344 with three of halves, 359 (V = 1)
+// with sections of odd length; 512 with Q and K turned in HBM.  The staged values are rounded to fp16
+// first, as the intermediates in HBM are.
+template <bool PAIRS, int V>
+__device__ __forceinline__ void turn_slots(const RopeGeom &g, const int4 *where, int n_slots, _Float16 *qk) {
+    constexpr int UNITS = SH_DH / 2 / V, W = PAIRS ? 2 * V : V;
+    typedef _Float16 Run __attribute__((ext_vector_type(W)));
+    const int p0 = threadIdx.x % UNITS * V;
+    if (p0 >= g.P) return;
+    int axis[V], lo, hi;
+    double turn[V], origin[V];
+    rope_channels(g, p0, lo, hi);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int p = min(p0 + j, g.P - 1);
+        axis[j] = rope_axis(g, p);
+        turn[j] = g.turn[p];
+        origin[j] = g.origin[axis[j]];
+    }
+    for (int b = threadIdx.x / UNITS; b < n_slots; b += 256 / UNITS) {
+        const int4 w = where[b];
+        if (!w.w) continue;   // (a row without a token is not turned)
+        _Float16 *const row = qk + b * QKS;
+        Run *const q = reinterpret_cast<Run *>(row + lo), *const k = reinterpret_cast<Run *>(row + SH_DH + lo);
+        Run *const qh = reinterpret_cast<Run *>(row + hi), *const kh = reinterpret_cast<Run *>(row + SH_DH + hi);
+        Run a = *q, c = *k, ah, ch;
+        if constexpr (!PAIRS) {
+            ah = *qh;
+            ch = *kh;
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (p0 + j >= g.P) break;   // (not turned)
+            const int at = axis[j] == 0 ? w.x : axis[j] == 1 ? w.y : w.z;
+            const Turn t = rope_turn16(rope_fraction(at, origin[j], turn[j]));
+            const int l = PAIRS ? 2 * j : j;
+            float q0 = (float)a[l], q1 = PAIRS ? (float)a[l + PAIRS] : (float)ah[j];
+            float k0 = (float)c[l], k1 = PAIRS ? (float)c[l + PAIRS] : (float)ch[j];
+            turn_pair(q0, q1, t);
+            turn_pair(k0, k1, t);
+            a[l] = (_Float16)q0;
+            c[l] = (_Float16)k0;
+            (PAIRS ? a : ah)[PAIRS ? l + 1 : j] = (_Float16)q1;
+            (PAIRS ? c : ch)[PAIRS ? l + 1 : j] = (_Float16)k1;
+        }
+        *q = a;
+        *k = c;
+        if constexpr (!PAIRS) {
+            *qh = ah;
+            *kh = ch;
+        }
+    }
+}
+
+template <typename ROPE>
 __global__ __launch_bounds__(256) void k_qkv_attn_short(RowMap rm, const uint16_t *__restrict__ wq,
                                                         const uint16_t *__restrict__ wk,
                                                         const uint16_t *__restrict__ wv, int hd, int heads,
                                                         int n_seq, int L, int s_t, int n_tiles, float qscale,
-                                                        uint16_t *__restrict__ O) {
+                                                        uint16_t *__restrict__ O, ROPE rp) {
     using T = ShortTile;
+    constexpr bool ROTATE = !std::is_same<ROPE, NoRope>::value;
     extern __shared__ __align__(16) uint16_t lds[];
     const int lid = xcd_remap(blockIdx.x, n_tiles * heads);
     const int h = lid % heads, tile = lid / heads;
@@ -76,6 +143,10 @@ __global__ __launch_bounds__(256) void k_qkv_attn_short(RowMap rm, const uint16_
         rb.base[i] = xb;
         rb.off[i] = (uint32_t)tok * (uint32_t)(C * 2) + (uint32_t)rb.chunk() * 16;
     }
+    long tok = -1;   // of slot threadIdx.x, for its position
+    if constexpr (ROTATE) {
+        if ((int)threadIdx.x < n_slots) tok = batch_token(seq0 * L + (int)threadIdx.x, rp.idx, rm.tF, rm.tN);
+    }
     T t;
     t.run(lds, ra, rb, C);
 
@@ -102,6 +173,28 @@ __global__ __launch_bounds__(256) void k_qkv_attn_short(RowMap rm, const uint16_
                     for (int e = 0; e < 4; ++e) VT[(a - 2 * SH_DH + e) * VTS + pos] = f2h_bits(t.acc[i][j][4 * g + e]);
                 }
             }
+    }
+    if constexpr (ROTATE) {
+        // ---- turn Q and K in place ----
+        int4 *const where = reinterpret_cast<int4 *>(lds + SH_STAGE_BYTES / 2);
+        if (threadIdx.x < 128) {
+            int4 w = {0, 0, 0, tok >= 0 && tok < rp.g.FN};
+            if (w.w) {
+                const int n = (int)tok % rp.g.N;
+                w.x = (int)tok / rp.g.N;
+                w.y = n / rp.g.W;
+                w.z = n % rp.g.W;
+            }
+            where[threadIdx.x] = w;
+        }
+        __syncthreads();
+        _Float16 *const qk = reinterpret_cast<_Float16 *>(QK);
+        if (rp.g.pairs)
+            turn_slots<true, 4>(rp.g, where, n_slots, qk);
+        else if (rp.g.vec >= 4)
+            turn_slots<false, 4>(rp.g, where, n_slots, qk);
+        else
+            turn_slots<false, 1>(rp.g, where, n_slots, qk);
     }
     __syncthreads();
 
@@ -189,8 +282,7 @@ __global__ __launch_bounds__(256) void k_qkv_attn_short(RowMap rm, const uint16_
 
 bool qkv_attn_short_applies(const Plan &p, const AttnArgs &a) {
     return p.bf16 && p.dh == SH_DH && p.C % 64 == 0 && a.n_ctx == 0 && a.seq_off == nullptr && a.n_seq >= 1 &&
-           a.L >= 1 && a.rope == nullptr &&
-           attn_short(a.L) && (long)a.n_seq * a.L < (1L << 31);
+           a.L >= 1 && attn_short(a.L) && (long)a.n_seq * a.L < (1L << 31);
 }
 
 hipError_t launch_qkv_attn_short(const Plan &p, const RowMap &rm, const AttnArgs &a, hipStream_t st) {
@@ -199,12 +291,16 @@ hipError_t launch_qkv_attn_short(const Plan &p, const RowMap &rm, const AttnArgs
     const int s_t = 128 / a.L;
     const int n_tiles = cdiv(a.n_seq, s_t);
     const float qscale = (float)(1.4426950408889634 / sqrt((double)p.dh));
-    const hipError_t e = raise_lds_limit((const void *)k_qkv_attn_short, ShortTile::LDS_BYTES);
-    if (e != hipSuccess) return e;
-    launch_k(k_qkv_attn_short, (unsigned)(n_tiles * p.heads), 256, ShortTile::LDS_BYTES, st, rm,
-             (const uint16_t *)a.wq, (const uint16_t *)a.wk, (const uint16_t *)a.wv, p.hd, p.heads, a.n_seq, a.L,
-             s_t, n_tiles, qscale, (uint16_t *)a.o);
-    return hipGetLastError();
+    auto go = [&](auto kern, const auto &rp) {
+        const hipError_t e = raise_lds_limit((const void *)kern, ShortTile::LDS_BYTES);
+        if (e != hipSuccess) return e;
+        launch_k(kern, (unsigned)(n_tiles * p.heads), 256, ShortTile::LDS_BYTES, st, rm, (const uint16_t *)a.wq,
+                 (const uint16_t *)a.wk, (const uint16_t *)a.wv, p.hd, p.heads, a.n_seq, a.L, s_t, n_tiles, qscale,
+                 (uint16_t *)a.o, rp);
+        return hipGetLastError();
+    };
+    if (a.rope == nullptr) return go(k_qkv_attn_short<NoRope>, NoRope{});
+    return go(k_qkv_attn_short<ShortRope>, ShortRope{*a.rope, a.rope_idx != nullptr ? a.rope_idx : a.row_idx});
 }
 
 }  // namespace oc

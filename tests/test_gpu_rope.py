@@ -248,6 +248,32 @@ def test_layer(i):
         bars(yf[q], ref[:len(q)], dt, "uncached rows")
 
 
+@pytest.mark.parametrize("L,n_seq", [(1, 130), (3, 43), (25, 11), (64, 3)])
+@pytest.mark.parametrize("rp", [oc.Rope((64, 0, 0)), oc.Rope((16, 24, 24), layout="halves", shared=True),
+                                oc.Rope((14, 10, 22)), oc.Rope((14, 10, 22), layout="halves"),
+                                oc.Rope((6, 0, 4), layout="split")])
+def test_short_sequences(rp, L, n_seq):
+    """Heads of 64 and few tokens a sequence; rows without a token are not turned."""
+    sh = oc.Shape(**GRID, C=128, heads=3, head_dim=64)
+    n = sh.F * sh.N
+    g = torch.Generator().manual_seed(L)
+    W64 = {k: torch.randn(192, 128, generator=g, dtype=torch.float64) / 128 ** 0.5 for k in ("wq", "wk", "wv")}
+    W64["wo"] = torch.randn(128, 192, generator=g, dtype=torch.float64) / 192 ** 0.5
+    W = {k: v.bfloat16().to(DEV) for k, v in W64.items()}
+    W64 = {k: v.cpu().double().numpy() for k, v in W.items()}
+    x = torch.randn(n_seq * L, 128, generator=g).bfloat16()
+    idx = torch.randint(0, n, (n_seq * L,), generator=g, dtype=torch.int32)
+    idx[::7] = n
+    idx[3::11] = -1
+    y, _ = oc.attn_reduced(x.to(DEV), n_seq, L, W, sh, rope=rp, kept_idx=idx.to(DEV))
+    there = (idx >= 0) & (idx < n)
+    pos = grid_pos(torch.where(there, idx, 0).long(), sh.H, sh.W)
+    pos[~there] = 0   # (the angle at the origin is nothing)
+    ref = np.concatenate([attention(x[i:i + L].double().numpy(), None, pos[i:i + L], W64, 3, 64, rp)
+                          for i in range(0, n_seq * L, L)])
+    bars(to_f64(y).reshape(ref.shape), ref, "bf16", "rows")
+
+
 def test_staged_calls_and_runner_match_the_layer_call():
     from paper_2607_23844_amd import runner
     gran, kw, rp = LAYERS[0]
