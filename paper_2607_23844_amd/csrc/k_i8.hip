@@ -157,10 +157,12 @@ hipError_t go_quant(const T *x, long ld, int n_src, int K, const int *idx, int r
     return c <= 1024 ? go(k_quant<T, 256, 4>, 1) : go(k_quant<T, 256, 0>, 1);
 }
 
-// GELU in its tanh form, v / (1 + exp(-2 z)) (exp and reciprocal to 1 ulp)
+// GELU in its tanh form, v / (1 + exp(-2 z)), z = sqrt(2/pi) (v + 0.044715 v^3)
+// (exp and reciprocal to 1 ulp)
 __device__ __forceinline__ float gelu_tanh(float v) {
-    const float z = 0.7978845608028654f * fmaf(0.044715f * v, v * v, v);
-    return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-2.8853900817779268f * z));
+    constexpr double c = -2.0 * 1.4426950408889634 * 0.7978845608028654;   // -2 z log2(e) = c v + 0.044715 c v^3
+    const float e = v * fmaf(v * v, (float)(c * 0.044715), (float)c);
+    return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(e));
 }
 
 // Scales and biases of four consecutive outputs, and these outputs of a row from
@@ -192,10 +194,17 @@ __device__ __forceinline__ f32x4 finish4(i32x4 acc, float sq, f32x4 sw, f32x4 b)
     return v;
 }
 __device__ __forceinline__ u16x4 to_bf16(f32x4 v) {
-    bf16x4 o;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (__bf16)v[e];
-    return *reinterpret_cast<u16x4 *>(&o);
+    return __builtin_bit_cast(u16x4, __builtin_convertvector(v, bf16x4));
+}
+
+// Exchanges x of lanes 16..31 and 48..63 with y of lanes 0..15 and 32..47.
+__device__ __forceinline__ void swap16(uint4 &x, uint4 &y) {
+    const auto a = __builtin_amdgcn_permlane16_swap(x.x, y.x, false, false);
+    const auto b = __builtin_amdgcn_permlane16_swap(x.y, y.y, false, false);
+    const auto c = __builtin_amdgcn_permlane16_swap(x.z, y.z, false, false);
+    const auto d = __builtin_amdgcn_permlane16_swap(x.w, y.w, false, false);
+    x = make_uint4(a[0], b[0], c[0], d[0]);
+    y = make_uint4(a[1], b[1], c[1], d[1]);
 }
 
 // Between a wave's writes and reads of LDS that no other wave touches.
@@ -212,16 +221,20 @@ __device__ __forceinline__ long out_row(const LinearI8Args &a, long r) {
 }
 
 // ---------------------------------------------------------------------------
-// The product on ring-buffered MFMA tiles: a = weight rows, b = batch rows.
-// bf16 tiles are staged through LDS and written in 16-byte chunks of whole
-// rows, fp32 tiles wave by wave.
+// The product on ring-buffered MFMA tiles: a = weight rows, b = batch rows.  A
+// lane of an accumulator of 32 x 32 has four outputs of one row in each of four
+// groups.  bf16: lanes exchange them (v_permlane32_swap, v_permlane16_swap) until
+// each stores 16 bytes of a row beside its partners', and waves finish one by
+// one; through LDS in whole rows, after a barrier, it took 73 us (now 63) for
+// 230400 x 320 x 320, 252 (246) x 1280, 330 (296) with GELU, 11.2 (10.0) for 2048
+// x 1536 x 1536 and 61 (57) for 4429 x 1536 x 6144 with GELU.  fp32: through LDS
+// wave by wave.
 // ---------------------------------------------------------------------------
-// LDS behind the staged rows: scales and biases of the outputs, scales and places
-// of the rows
+// LDS: the ring, or in its place scales and biases of the outputs, scales and
+// places of the rows, and the waves' parts for fp32
+constexpr int F32_LD = 36;
 template <typename R>
-constexpr size_t LIN_STAGE = std::max<size_t>((size_t)R::BB * (R::BA + 8) * 2, R::NW * 32 * 36 * 4);
-template <typename R>
-constexpr size_t LIN_LDS = std::max<size_t>(R::LDS_BYTES, LIN_STAGE<R> + (R::BA + R::BB) * 8);
+constexpr size_t LIN_LDS = std::max<size_t>(R::RING_BYTES, (R::BA + R::BB) * 8 + R::NW * 32 * F32_LD * 4);
 
 template <int ID, typename T, bool GELU>
 __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, int n_at, int n_bt) {
@@ -251,7 +264,8 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, 
     ring_rows(rb, (const uint16_t *)a.q, a.rows, K2, b0);
     R t;
     t.run(lds, ra, rb, K2);
-    float *const col_sw = reinterpret_cast<float *>(reinterpret_cast<char *>(lds) + LIN_STAGE<R>), *const col_b = col_sw + BA;
+    // (in the ring, free now)
+    float *const col_sw = reinterpret_cast<float *>(lds), *const col_b = col_sw + BA;
     float *const row_sq = col_b + BA;
     int *const row_out = reinterpret_cast<int *>(row_sq + BB);   // y row, or -1
     if ((int)threadIdx.x < BA) {
@@ -263,33 +277,57 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, 
         row_out[threadIdx.x] = b0 + (int)threadIdx.x < a.rows && my_out >= 0 && my_out < a.n_out ? my_out : -1;
     }
     __syncthreads();
+    const int lane = threadIdx.x & 63;
     float sq[R::TB];
 #pragma unroll
     for (int j = 0; j < R::TB; ++j) sq[j] = row_sq[R::b_of(j)];
     if constexpr (sizeof(T) == 2) {
+        // 32 bytes of a row together with GELU, whose stores come further apart, 64 without (230400 x 320 x
+        // 1280: 300 us against 310, 258 against 272)
+        constexpr int ROWS = GELU ? 1 : 2;   // rows that a lane stores of an accumulator
 #pragma unroll
-        for (int i = 0; i < R::TA; ++i)
+        for (int j = 0; j < R::TB; ++j) {
+            uint16_t *to[ROWS];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int n = R::a_of(i, g);
-                const f32x4 sw = *reinterpret_cast<const f32x4 *>(col_sw + n), bias = *reinterpret_cast<const f32x4 *>(col_b + n);
-#pragma unroll
-                for (int j = 0; j < R::TB; ++j)
-                    *reinterpret_cast<u16x4 *>(lds + R::b_of(j) * (BA + 8) + n) =
-                        to_bf16(finish4<GELU>(four(t.acc[i][j], g), sq[j], sw, bias));
+            for (int h = 0; h < ROWS; ++h) {
+                const int o = row_out[(R::b_of(j) & ~31) + (lane & (32 / ROWS - 1)) + h * (32 / ROWS)];
+                to[h] = o >= 0 ? (uint16_t *)a.y + o * a.ld_y : nullptr;
             }
-        __syncthreads();
-        write_rows<BA, BB, R::NT>(lds, min(BA, a.N - a0), [&](int b, int c0) -> uint16_t * {
-            const int o = row_out[b];
-            return o >= 0 ? (uint16_t *)a.y + o * a.ld_y + a0 + c0 : nullptr;
-        });
+            auto store = [&](int h, int n, uint4 v) {
+                if (to[h] != nullptr && n < a.N) *reinterpret_cast<uint4 *>(to[h] + n) = v;
+            };
+#pragma unroll
+            for (int i = 0; i < R::TA; ++i) {
+                auto group = [&](int g) {
+                    const int c = R::a_of(i, g);
+                    return __builtin_bit_cast(
+                        uint2, to_bf16(finish4<GELU>(four(t.acc[i][j], g), sq[j], *reinterpret_cast<const f32x4 *>(col_sw + c),
+                                                     *reinterpret_cast<const f32x4 *>(col_b + c))));
+                };
+                uint4 v[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {   // outputs 0..7 | 8..15 in the halves of the wave, and 16 further
+                    const uint2 x = group(2 * h), y = group(2 * h + 1);
+                    const auto p = __builtin_amdgcn_permlane32_swap(x.x, y.x, false, false);
+                    const auto q = __builtin_amdgcn_permlane32_swap(x.y, y.y, false, false);
+                    v[h] = make_uint4(p[0], q[0], p[1], q[1]);
+                }
+                const int n = a0 + (R::a_of(i, 0) & ~31) + (lane & 32) / 4;
+                if constexpr (ROWS == 2) {
+                    swap16(v[0], v[1]);
+                    store(0, n + (lane & 16), v[0]);
+                    store(1, n + (lane & 16), v[1]);
+                } else {
+                    store(0, n, v[0]);
+                    store(0, n + 16, v[1]);
+                }
+            }
+        }
     } else {
         // 32 rows of 32 outputs at a time through a part of LDS of the wave's own: 128 bytes of a row
-        // are stored together (each lane storing its four outputs took 80 us for 4429 x 1536 x 6144)
-        constexpr int LD = 36;
-        const int lane = threadIdx.x & 63;
-        float *const mine = reinterpret_cast<float *>(lds) + (threadIdx.x >> 6) * 32 * LD;
-        static_assert(LIN_STAGE<R> >= R::NW * 32 * LD * 4, "the waves' parts");
+        // are stored together (each lane storing its four outputs took 80 us for 4429 x 1536 x 6144; 128 bytes
+        // exchanged between lanes as above 59, this 56: there the neighbours of a store are lanes apart)
+        float *const mine = reinterpret_cast<float *>(row_out + BB) + (threadIdx.x >> 6) * 32 * F32_LD;
 #pragma unroll
         for (int i = 0; i < R::TA; ++i) {
             const int n = a0 + (R::a_of(i, 0) & ~31) + (lane & 7) * 4;   // outputs that this lane stores
@@ -298,7 +336,7 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, 
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int c = R::a_of(i, g);
-                    *reinterpret_cast<f32x4 *>(mine + (lane & 31) * LD + 8 * g + 4 * (lane >> 5)) =
+                    *reinterpret_cast<f32x4 *>(mine + (lane & 31) * F32_LD + 8 * g + 4 * (lane >> 5)) =
                         finish4<GELU>(four(t.acc[i][j], g), sq[j], *reinterpret_cast<const f32x4 *>(col_sw + c),
                                       *reinterpret_cast<const f32x4 *>(col_b + c));
                 }
@@ -306,7 +344,7 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, 
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int r = k * 8 + (lane >> 3);
-                    const f32x4 v = *reinterpret_cast<const f32x4 *>(mine + r * LD + (lane & 7) * 4);
+                    const f32x4 v = *reinterpret_cast<const f32x4 *>(mine + r * F32_LD + (lane & 7) * 4);
                     const int o = row_out[(R::b_of(j) & ~31) + r];
                     if (o >= 0 && n < a.N) *reinterpret_cast<f32x4 *>((T *)a.y + o * a.ld_y + n) = v;
                 }

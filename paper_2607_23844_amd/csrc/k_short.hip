@@ -12,8 +12,9 @@
 // fp32 accumulation; Q scaled by log2(e)/sqrt(dh)).  The epilogue stages Q
 // and K by slot rows and V transposed (d rows, slot positions permuted inside
 // 16-slot blocks as the Vt layout of the long-sequence kernels), all fp16 in
-// LDS, where a layer with rotary positions turns them.  Each wave then takes 32 query slots: S^T = K Q^T over the 32-slot key
-// blocks that hold its queries' sequences, keys of other sequences masked,
+// LDS, where a layer with rotary positions turns Q and K.  Each wave then takes
+// 32 query slots: S^T = K Q^T over the 32-slot key blocks that hold its
+// queries' sequences, keys of other sequences masked,
 // the exact maximum, P = exp2(s - max) in fp16, the running sum of that
 // fp16 P, O^T = Vt P^T, and O = O^T / sum written by rows [rows, H*dh].
 #include "oc_internal.h"
