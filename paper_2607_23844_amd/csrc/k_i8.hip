@@ -425,16 +425,16 @@ hipError_t go_thin(const LinearI8Args &a, hipStream_t st) {
 
 // The tile shapes' costs for this product (as RING_SHAPES; its epilogue is
 // longer, in 8 bits a step is 128 elements).  Least squares over 64 products of
-// 33 to 230400 rows, K and N of 64 to 6144, with and without GELU in bf16 and in
-// fp32: the shape picked is 0.5, 1.4 and 1.1% slower than the fastest on the
-// average (30% at worst); with the figures of the 16-bit projections 4.1, 5.7
-// and 4.4% (48%).
+// 33 to 230400 rows, K and N of 64 to 6144, with and without GELU in bf16: the
+// shape picked is 0.9% slower than the fastest on the average (20% at worst), in
+// fp32 0.9 (27%); with the figures of the 16-bit projections 2.6, with GELU 3.6
+// and in fp32 4.2% (40%).
 constexpr RingShapeCost I8_SHAPES[N_RING_SHAPES] = {
-    {256, 256, 1, 7.61f, {1.235f}},         {256, 192, 1, 6.10f, {0.988f}},
-    {256, 128, 1, 4.76f, {0.766f}},         {128, 192, 1, 5.14f, {0.639f}},
-    {96, 128, 1, 3.59f, {0.430f}},          {128, 128, 2, 3.66f, {0.498f, 1.152f}},
-    {128, 192, 2, 5.01f, {0.606f, 1.441f}}, {160, 128, 2, 4.74f, {0.571f, 1.310f}},
-    {64, 64, 3, 1.95f, {0.264f, 0.481f, 0.618f}}, {128, 64, 2, 2.67f, {0.352f, 0.679f}},
+    {256, 256, 1, 6.09f, {1.252f}},         {256, 192, 1, 4.95f, {0.997f}},
+    {256, 128, 1, 3.91f, {0.772f}},         {128, 192, 1, 3.92f, {0.638f}},
+    {96, 128, 1, 2.65f, {0.434f}},          {128, 128, 2, 2.79f, {0.494f, 1.146f}},
+    {128, 192, 2, 3.76f, {0.599f, 1.451f}}, {160, 128, 2, 3.12f, {0.575f, 1.326f}},
+    {64, 64, 3, 1.63f, {0.267f, 0.462f, 0.625f}}, {128, 64, 2, 2.11f, {0.356f, 0.689f}},
 };
 
 template <typename T, bool GELU>
