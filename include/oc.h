@@ -514,10 +514,9 @@ oc_status oc_rope_qk(const oc_shape *shape, const oc_rope *rope, int32_t n_rows,
  * exactly the call without it.  oc_attn_reduced_rope takes the tokens of its
  * rows: kept_idx [n_seq * seq_len], as oc_gather got it (rows outside [0, F*N)
  * are not turned).  bf16 layers hold q and k in fp16 before and after the
- * rotation (a second rounding of 2^-11); head_dim 64 layers of short
- * sequences give up the fused projection and attention for it.  Workspaces
- * as without _rope.  (oc_layer_cached_static and oc_block_cached have no such
- * form: a block with positions is two oc_layer_cached_rope calls and
+ * rotation (a second rounding of 2^-11).  Workspaces as without _rope.
+ * (oc_layer_cached_static and oc_block_cached have no such form: a block with
+ * positions is two oc_layer_cached_rope calls and
  * oc_residual_add or oc_norm_gate between them.)
  */
 oc_status oc_attn_reduced_rope(const oc_shape *shape, const oc_rope *rope, const int32_t *kept_idx,
@@ -569,10 +568,10 @@ typedef enum { OC_ACT_NONE = 0, OC_ACT_GELU = 1 } oc_act;   /* GELU: the tanh fo
  * sums are exact 32-bit integers, the rest fp32, rounded once to y's type
  * dtype (also that of bias, which may be NULL).  Rows of y are ld_y elements
  * apart; rows t_r outside [0, n_out) are not written, nor any other row.  The
- * same t_r twice: either row is kept.
- * K as in oc_quant_rows, N a multiple of 8, n_rows * N < 2^37; q, w, scale_w, bias and y 16-byte
- * aligned, ld_y >= N and a multiple of 16 bytes, y overlaps no input; without
- * out_idx, n_rows <= n_out.
+ * same t_r twice: each output is that of one of the rows.
+ * K as in oc_quant_rows, N a multiple of 8, n_rows * N < 2^37; q, w, scale_w,
+ * bias and y 16-byte aligned, ld_y >= N and a multiple of 16 bytes, y overlaps
+ * no input; without out_idx, n_rows <= n_out.
  */
 oc_status oc_linear_i8(int32_t dtype, int32_t n_rows, int32_t K, int32_t N, const int8_t *q, const float *scale_q,
                        const int8_t *w, const float *scale_w, const void *bias, int32_t act, const int32_t *out_idx,
