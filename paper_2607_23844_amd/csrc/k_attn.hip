@@ -336,8 +336,9 @@ hipError_t launch_attention(const Plan &p, const AttnArgs &a, hipStream_t st) {
             if ((e = launch_qkv_attn_short(p, rm, a, st)) != hipSuccess) return e;
             return launch_proj_out(p, n_rows, a, st);
         }
-        e = launch_proj_qkv(p, rm, a, st);   // (converts wo when no earlier launch has)
-        if (e != hipSuccess || (e = rotate_qk(p, a, st)) != hipSuccess) return e;
+        bool rotated;
+        e = launch_proj_qkv(p, rm, a, st, rotated);   // (converts wo when no earlier launch has)
+        if (e != hipSuccess || (!rotated && (e = rotate_qk(p, a, st)) != hipSuccess)) return e;
         if ((e = launch_flash(p, a, Lk, st)) != hipSuccess) return e;
         AttnArgs o = a;
         o.wo16_ready = 1;

@@ -33,6 +33,7 @@
 #include "oc_attn_common.h"
 #include "oc_gemm_epi.h"
 #include "oc_ring_tile.h"
+#include "oc_rope.h"
 #include <algorithm>
 
 namespace oc {
@@ -80,6 +81,51 @@ __device__ __forceinline__ void to_f16(const uint4 *__restrict__ src, long n8, u
     }
 }
 
+// Rotary positions are applied to the staged rows of Q and K, where the halves
+// of a head lie in one tile: a thread takes four pairs of a row, makes their
+// angles once and turns these pairs of every head in the tile.  Cached layers,
+// without rotation / with it here / with a pass of its own over Q and K: 2381
+// rows, 24 heads of 64 139 / 142.5 / 147 us; 25 x 72 x 128 tokens with patches of
+// 4 x 4, 5 heads of 64 836 / 855 / 880; 16 frames of 256 tokens, 16 heads of 72,
+// 71.5 / 74.5 / 80.
+static bool rope_in_tile(const RopeGeom &g, int BA) { return g.vec >= 4 && (g.pairs || BA % g.dh == 0); }
+template <typename T>
+constexpr size_t PROJ_ROPE_LDS = std::max<size_t>(T::LDS_BYTES, (size_t)T::BB * (T::BA + 8) * 2 + T::BB * 16);
+
+template <bool PAIRS, int BA, int BB, int NT>
+__device__ __forceinline__ void turn_rows(const RopeGeom &g, const int4 *where, int a0, int n_cols, uint16_t *S) {
+    constexpr int SROW = BA + 8;
+    // thread u of a row: the tile's 8 channels from 8 u on, or four pairs of the head that they lie in, and the same of
+    // every other head
+    const int per_head = g.dh / 8, step = NT / per_head, first = threadIdx.x / per_head, u = threadIdx.x - first * per_head;
+    if (first >= step || u * 8 >= n_cols) return;
+    const int d = (a0 + u * 8) % g.dh, p0 = d / 2, head = u * 8 - d;   // (PAIRS: it may begin before the tile)
+    if (p0 >= g.P) return;
+    const RopeUnit<PAIRS, 4> unit(g, p0);
+    for (int b = first; b < BB; b += step) {
+        const int4 w = where[b];
+        if (!w.w) continue;   // (a row without a token is not turned)
+        Turn t[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[j] = unit.at(w, j);
+        _Float16 *const row = reinterpret_cast<_Float16 *>(S + b * SROW) + head;
+        constexpr int N = 4;   // heads at a time
+        for (int c = u * 8; c < n_cols; c += N * g.dh) {
+            typename RopeUnit<PAIRS, 4>::Vals v[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (c + i * g.dh < n_cols) v[i] = unit.load(row + c - u * 8 + i * g.dh);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (c + i * g.dh >= n_cols) break;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) unit.apply(v[i], j, t[j]);
+                unit.store(row + c - u * 8 + i * g.dh, v[i]);
+            }
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Q, K and V in one launch.  The first n_qk tiles are row tiles: a in [0,
 // nw*hd) are rows of wq, wk (and wv when nw = 3), b = batch rows, staged as
@@ -96,12 +142,12 @@ __device__ __forceinline__ void to_f16(const uint4 *__restrict__ src, long n8, u
 // the call has (the uncached layer and the attention entry point: a launch of
 // its own took 4.5 us of 263 on the SD3-like layer, 4.4 of 220 by stages).
 // ---------------------------------------------------------------------------
-template <int ID>
+template <int ID, typename ROPE>
 __global__ __launch_bounds__(RING_THREADS<ID>) void k_proj_qkv(
     RowMap rm, const uint16_t *__restrict__ wq, const uint16_t *__restrict__ wk, const uint16_t *__restrict__ wv,
     int hd, int dh, float qscale, int nw, int n_qk_at, int n_bt, int n_v_at, int n_v_bt, int n_seq, int L, int lpad,
     int zero_pad, const int32_t *__restrict__ seq_off, uint16_t *__restrict__ Q, uint16_t *__restrict__ K,
-    uint16_t *__restrict__ Vt, const uint4 *__restrict__ wo, long n8, uint4 *__restrict__ wo16) {
+    uint16_t *__restrict__ Vt, const uint4 *__restrict__ wo, long n8, uint4 *__restrict__ wo16, ROPE rp) {
     using T = typename RingShape<ID, RING_BF16>::Tile;
     constexpr int BA = T::BA, BB = T::BB, NT = T::NT;
     extern __shared__ __align__(16) uint16_t lds[];
@@ -120,9 +166,22 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_proj_qkv(
         const int a0 = at * BA, b0 = bt * BB;
         ring_rows3(ra, wq, wk, wv, hd, nw * hd, rm.C, a0);
         ring_batch_rows(rb, rm, b0);
+        static_assert(BB <= NT, "a thread for each row");
+        long tok = -1;   // of row threadIdx.x of the tile, for its position
+        if constexpr (ROTATES<ROPE>) {
+            const int r = b0 + (int)threadIdx.x;
+            if ((int)threadIdx.x < BB && r < rm.n_main) tok = batch_token(r, rp.idx, rm.tF, rm.tN);
+        }
         t.run(lds, ra, rb, rm.C);
         stage_rows<BA>(t, lds, [&](float v, int a) { return f2h_bits(a0 + a < hd ? v * qscale : v); },
                        [](int a) { return a; });
+        if constexpr (ROTATES<ROPE>) {
+            int4 *const where = reinterpret_cast<int4 *>(lds + BB * (BA + 8));
+            if ((int)threadIdx.x < BB) where[threadIdx.x] = rope_place(rp.g, tok);
+            __syncthreads();
+            if (rp.g.pairs) turn_rows<true, BA, BB, NT>(rp.g, where, a0, min(BA, 2 * hd - a0), lds);
+            else turn_rows<false, BA, BB, NT>(rp.g, where, a0, min(BA, 2 * hd - a0), lds);
+        }
         __syncthreads();
         write_rows<BA, BB, NT>(lds, min(BA, nw * hd - a0), [&](int b, int c0) -> uint16_t * {
             const int r = b0 + b, a = a0 + c0;
@@ -212,7 +271,8 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_proj_qkv(
     }
 }
 
-hipError_t launch_proj_qkv(const Plan &p, const RowMap &rm, const AttnArgs &a, hipStream_t st) {
+hipError_t launch_proj_qkv(const Plan &p, const RowMap &rm, const AttnArgs &a, hipStream_t st, bool &rotated) {
+    rotated = false;
     const float qscale = (float)(1.4426950408889634 / sqrt((double)p.dh));
     StageScope _stage(st, "proj_qkv");
     const int Lk = a.n_seq == 1 ? rm.n_rows : a.L;
@@ -227,16 +287,21 @@ hipError_t launch_proj_qkv(const Plan &p, const RowMap &rm, const AttnArgs &a, h
     return ring_dispatch(id, [&](auto c) -> hipError_t {
         constexpr int ID = decltype(c)::value;
         using T = typename RingShape<ID, RING_BF16>::Tile;
-        const hipError_t e = allow_lds(k_proj_qkv<ID>, T::LDS_BYTES);
-        if (e != hipSuccess) return e;
         const int n_qk_at = cdiv(nw * p.hd, T::BA), n_bt = cdiv(rm.n_rows, T::BB);
         const int n_v_at = v_at(T::BA), n_v_bt = nw == 3 ? 0 : cdiv(p.hd, T::BB);
         const int cvt_blocks = (int)std::min<long>((n8 + 4 * T::NT - 1) / (4 * T::NT), N_CUS);
-        launch_k(k_proj_qkv<ID>, n_qk_at * n_bt + n_v_at * n_v_bt + cvt_blocks, T::NT, T::LDS_BYTES, st, rm,
-                 (const uint16_t *)a.wq, (const uint16_t *)a.wk, (const uint16_t *)a.wv, p.hd, p.dh, qscale, nw,
-                 n_qk_at, n_bt, n_v_at, n_v_bt, a.n_seq, a.L, a.lpad, zero_pad, a.seq_off, (uint16_t *)a.q, (uint16_t *)a.k,
-                 (uint16_t *)a.vt, (const uint4 *)a.wo, n8, (uint4 *)a.wo16);
-        return hipGetLastError();
+        auto go = [&](auto kern, size_t lds, const auto &rp) {
+            const hipError_t e = allow_lds(kern, lds);
+            if (e != hipSuccess) return e;
+            launch_k(kern, n_qk_at * n_bt + n_v_at * n_v_bt + cvt_blocks, T::NT, lds, st, rm, (const uint16_t *)a.wq,
+                     (const uint16_t *)a.wk, (const uint16_t *)a.wv, p.hd, p.dh, qscale, nw, n_qk_at, n_bt, n_v_at,
+                     n_v_bt, a.n_seq, a.L, a.lpad, zero_pad, a.seq_off, (uint16_t *)a.q, (uint16_t *)a.k,
+                     (uint16_t *)a.vt, (const uint4 *)a.wo, n8, (uint4 *)a.wo16, rp);
+            return hipGetLastError();
+        };
+        if (a.rope == nullptr || !rope_in_tile(*a.rope, T::BA)) return go(k_proj_qkv<ID, NoRope>, T::LDS_BYTES, NoRope{});
+        rotated = true;
+        return go(k_proj_qkv<ID, StagedRope>, PROJ_ROPE_LDS<T>, staged_rope(a));
     });
 }
 

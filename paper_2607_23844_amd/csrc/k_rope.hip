@@ -47,14 +47,11 @@ __device__ __forceinline__ void make_turns(const RopeGeom &g, const RopeArgs &a,
             for (int i = 0; i < 3; ++i) w[i] = a.pos[row * 3 + i];
             w[3] = 1;
         } else {
-            const long t = batch_token((int)row, a.idx, a.tF, a.tN);
-            w[3] = t >= 0 && t < g.FN;
-            if (w[3]) {   // (fewer than 2^30 tokens)
-                const int f = (int)t / g.N, n = (int)t - f * g.N;
-                w[0] = f;
-                w[1] = n / g.W;
-                w[2] = n % g.W;
-            }
+            const int4 at = rope_place(g, batch_token((int)row, a.idx, a.tF, a.tN));
+            w[0] = at.x;
+            w[1] = at.y;
+            w[2] = at.z;
+            w[3] = at.w;
         }
     }
     __syncthreads();

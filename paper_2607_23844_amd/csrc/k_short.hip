@@ -39,67 +39,31 @@ constexpr size_t SH_STAGE_BYTES = (size_t)(128 * QKS + SH_DH * VTS) * 2;
 static_assert(SH_STAGE_BYTES % 16 == 0 && SH_STAGE_BYTES + 128 * 16 <= ShortTile::LDS_BYTES, "staging fits in the ring");
 }  // namespace
 
-// The rotation of Q and K (ROPE) and its row -> token table, if not rm's.
-struct NoRope {};
-struct ShortRope {
-    RopeGeom g;
-    const int *idx;
-};
-
 // Turns the staged Q and K of the block's slots in place: a thread takes V pairs
 // of a slot's Q and K, so an angle is made once for the two, and their channels
 // in runs.  A cached layer of 25 x 72 x 128 tokens, 5 heads: 320 us without the
-// rotation, 336 with one axis of pairs, 344 with three of halves, 359 (V = 1)
+// rotation, 337 with one axis of pairs, 338 with three of halves, 360 (V = 1)
 // with sections of odd length; 512 with Q and K turned in HBM.  The staged values are rounded to fp16
 // first, as the intermediates in HBM are.
 template <bool PAIRS, int V>
 __device__ __forceinline__ void turn_slots(const RopeGeom &g, const int4 *where, int n_slots, _Float16 *qk) {
-    constexpr int UNITS = SH_DH / 2 / V, W = PAIRS ? 2 * V : V;
-    typedef _Float16 Run __attribute__((ext_vector_type(W)));
+    constexpr int UNITS = SH_DH / 2 / V;
     const int p0 = threadIdx.x % UNITS * V;
     if (p0 >= g.P) return;
-    int axis[V], lo, hi;
-    double turn[V], origin[V];
-    rope_channels(g, p0, lo, hi);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int p = min(p0 + j, g.P - 1);
-        axis[j] = rope_axis(g, p);
-        turn[j] = g.turn[p];
-        origin[j] = g.origin[axis[j]];
-    }
+    const RopeUnit<PAIRS, V> unit(g, p0);
     for (int b = threadIdx.x / UNITS; b < n_slots; b += 256 / UNITS) {
         const int4 w = where[b];
         if (!w.w) continue;   // (a row without a token is not turned)
-        _Float16 *const row = qk + b * QKS;
-        Run *const q = reinterpret_cast<Run *>(row + lo), *const k = reinterpret_cast<Run *>(row + SH_DH + lo);
-        Run *const qh = reinterpret_cast<Run *>(row + hi), *const kh = reinterpret_cast<Run *>(row + SH_DH + hi);
-        Run a = *q, c = *k, ah, ch;
-        if constexpr (!PAIRS) {
-            ah = *qh;
-            ch = *kh;
-        }
+        _Float16 *const q = qk + b * QKS, *const k = q + SH_DH;
+        auto vq = unit.load(q), vk = unit.load(k);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            if (p0 + j >= g.P) break;   // (not turned)
-            const int at = axis[j] == 0 ? w.x : axis[j] == 1 ? w.y : w.z;
-            const Turn t = rope_turn16(rope_fraction(at, origin[j], turn[j]));
-            const int l = PAIRS ? 2 * j : j;
-            float q0 = (float)a[l], q1 = PAIRS ? (float)a[l + PAIRS] : (float)ah[j];
-            float k0 = (float)c[l], k1 = PAIRS ? (float)c[l + PAIRS] : (float)ch[j];
-            turn_pair(q0, q1, t);
-            turn_pair(k0, k1, t);
-            a[l] = (_Float16)q0;
-            c[l] = (_Float16)k0;
-            (PAIRS ? a : ah)[PAIRS ? l + 1 : j] = (_Float16)q1;
-            (PAIRS ? c : ch)[PAIRS ? l + 1 : j] = (_Float16)k1;
+            const Turn t = unit.at(w, j);
+            unit.apply(vq, j, t);
+            unit.apply(vk, j, t);
         }
-        *q = a;
-        *k = c;
-        if constexpr (!PAIRS) {
-            *qh = ah;
-            *kh = ch;
-        }
+        unit.store(q, vq);
+        unit.store(k, vk);
     }
 }
 
@@ -110,7 +74,6 @@ __global__ __launch_bounds__(256) void k_qkv_attn_short(RowMap rm, const uint16_
                                                         int n_seq, int L, int s_t, int n_tiles, float qscale,
                                                         uint16_t *__restrict__ O, ROPE rp) {
     using T = ShortTile;
-    constexpr bool ROTATE = !std::is_same<ROPE, NoRope>::value;
     extern __shared__ __align__(16) uint16_t lds[];
     const int lid = xcd_remap(blockIdx.x, n_tiles * heads);
     const int h = lid % heads, tile = lid / heads;
@@ -145,7 +108,7 @@ __global__ __launch_bounds__(256) void k_qkv_attn_short(RowMap rm, const uint16_
         rb.off[i] = (uint32_t)tok * (uint32_t)(C * 2) + (uint32_t)rb.chunk() * 16;
     }
     long tok = -1;   // of slot threadIdx.x, for its position
-    if constexpr (ROTATE) {
+    if constexpr (ROTATES<ROPE>) {
         if ((int)threadIdx.x < n_slots) tok = batch_token(seq0 * L + (int)threadIdx.x, rp.idx, rm.tF, rm.tN);
     }
     T t;
@@ -175,27 +138,18 @@ __global__ __launch_bounds__(256) void k_qkv_attn_short(RowMap rm, const uint16_
                 }
             }
     }
-    if constexpr (ROTATE) {
+    if constexpr (ROTATES<ROPE>) {
         // ---- turn Q and K in place ----
         int4 *const where = reinterpret_cast<int4 *>(lds + SH_STAGE_BYTES / 2);
-        if (threadIdx.x < 128) {
-            int4 w = {0, 0, 0, tok >= 0 && tok < rp.g.FN};
-            if (w.w) {
-                const int n = (int)tok % rp.g.N;
-                w.x = (int)tok / rp.g.N;
-                w.y = n / rp.g.W;
-                w.z = n % rp.g.W;
-            }
-            where[threadIdx.x] = w;
-        }
+        if (threadIdx.x < 128) where[threadIdx.x] = rope_place(rp.g, tok);
         __syncthreads();
         _Float16 *const qk = reinterpret_cast<_Float16 *>(QK);
-        if (rp.g.pairs)
-            turn_slots<true, 4>(rp.g, where, n_slots, qk);
-        else if (rp.g.vec >= 4)
-            turn_slots<false, 4>(rp.g, where, n_slots, qk);
-        else
+        if (rp.g.vec < 4)
             turn_slots<false, 1>(rp.g, where, n_slots, qk);
+        else if (rp.g.pairs)
+            turn_slots<true, 4>(rp.g, where, n_slots, qk);
+        else
+            turn_slots<false, 4>(rp.g, where, n_slots, qk);
     }
     __syncthreads();
 
@@ -301,7 +255,7 @@ hipError_t launch_qkv_attn_short(const Plan &p, const RowMap &rm, const AttnArgs
         return hipGetLastError();
     };
     if (a.rope == nullptr) return go(k_qkv_attn_short<NoRope>, NoRope{});
-    return go(k_qkv_attn_short<ShortRope>, ShortRope{*a.rope, a.rope_idx != nullptr ? a.rope_idx : a.row_idx});
+    return go(k_qkv_attn_short<StagedRope>, staged_rope(a));
 }
 
 }  // namespace oc

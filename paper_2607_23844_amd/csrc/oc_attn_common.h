@@ -93,7 +93,8 @@ constexpr int N_CUS = 256;
 bool qkv_attn_short_applies(const Plan &p, const AttnArgs &a);
 hipError_t launch_qkv_attn_short(const Plan &p, const RowMap &rm, const AttnArgs &a, hipStream_t st);
 
-hipError_t launch_proj_qkv(const Plan &p, const RowMap &rm, const AttnArgs &a, hipStream_t st);
+// (rotated: whether Q and K have been turned by a.rope)
+hipError_t launch_proj_qkv(const Plan &p, const RowMap &rm, const AttnArgs &a, hipStream_t st, bool &rotated);
 hipError_t launch_proj_out(const Plan &p, int n_rows, const AttnArgs &a, hipStream_t st);
 // Attention of few query tiles over long sequences: the waves of a block
 // share out the keys (k_flash_split.hip), where flash_splits says so

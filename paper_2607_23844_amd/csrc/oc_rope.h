@@ -1,7 +1,10 @@
-// Turning pairs of channels by a position (k_rope.hip, k_short.hip).
+// Turning pairs of channels by a position (k_rope.hip, and where k_short.hip and
+// k_proj.hip have staged Q and K).
 #pragma once
 #include "oc_device.h"
+#include "oc_internal.h"
 #include "oc_ops.h"
+#include <type_traits>
 
 namespace oc {
 
@@ -41,6 +44,75 @@ __device__ __forceinline__ void turn_pair(float &x, float &y, const Turn &t) {
     const float x0 = x, y0 = y;
     x = fmaf(x0, t.c, -(y0 * t.s));
     y = fmaf(x0, t.s, y0 * t.c);
+}
+
+// V pairs of a head, from pair p0 on (all of them turned), staged in LDS in fp16:
+// a run of 2 V channels, or two of V.  V = 1, or 4 where it divides the sections
+// (vec).
+template <bool PAIRS, int V>
+struct RopeUnit {
+    static constexpr int W = PAIRS ? 2 * V : V;
+    typedef _Float16 Run __attribute__((ext_vector_type(W)));
+    struct Vals { Run a, b; };
+    int lo, hi;                  // first channels
+    int on_x[V], on_y[V], on_z[V];   // masks of a pair's axis (selects became branches)
+    double turn[V], origin[V];
+    __device__ __forceinline__ RopeUnit(const RopeGeom &g, int p0) {
+        rope_channels(g, p0, lo, hi);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int axis = rope_axis(g, p0 + j);
+            on_x[j] = -(axis == 0);
+            on_y[j] = -(axis == 1);
+            on_z[j] = -(axis == 2);
+            turn[j] = g.turn[p0 + j];
+            origin[j] = g.origin[axis];
+        }
+    }
+    __device__ __forceinline__ Vals load(const _Float16 *head) const {
+        Vals v;
+        v.a = *reinterpret_cast<const Run *>(head + lo);
+        if constexpr (!PAIRS) v.b = *reinterpret_cast<const Run *>(head + hi);
+        return v;
+    }
+    __device__ __forceinline__ void store(_Float16 *head, const Vals &v) const {
+        *reinterpret_cast<Run *>(head + lo) = v.a;
+        if constexpr (!PAIRS) *reinterpret_cast<Run *>(head + hi) = v.b;
+    }
+    // pair j's angle at frame w.x, row w.y, column w.z
+    __device__ __forceinline__ Turn at(const int4 &w, int j) const {
+        return rope_turn16(rope_fraction((w.x & on_x[j]) | (w.y & on_y[j]) | (w.z & on_z[j]), origin[j], turn[j]));
+    }
+    __device__ __forceinline__ static void apply(Vals &v, int j, const Turn &t) {
+        float x = (float)v.a[PAIRS ? 2 * j : j], y = PAIRS ? (float)v.a[PAIRS ? 2 * j + 1 : 0] : (float)v.b[j];
+        turn_pair(x, y, t);
+        v.a[PAIRS ? 2 * j : j] = (_Float16)x;
+        (PAIRS ? v.a : v.b)[PAIRS ? 2 * j + 1 : j] = (_Float16)y;
+    }
+};
+
+// Where token t of the grid lies (w = 0: it has no place)
+__device__ __forceinline__ int4 rope_place(const RopeGeom &g, long t) {
+    int4 w = {0, 0, 0, t >= 0 && t < g.FN};
+    if (w.w) {   // (fewer than 2^30 tokens)
+        const int n = (int)t % g.N;
+        w.x = (int)t / g.N;
+        w.y = n / g.W;
+        w.z = n % g.W;
+    }
+    return w;
+}
+
+// Last argument of a kernel that stages Q and K: no rotation, or this one and its
+// row -> token table (NULL: as the rows are read).
+struct NoRope {};
+struct StagedRope {
+    RopeGeom g;
+    const int32_t *idx;
+};
+template <typename ROPE> constexpr bool ROTATES = std::is_same<ROPE, StagedRope>::value;
+inline StagedRope staged_rope(const AttnArgs &a) {
+    return StagedRope{*a.rope, a.rope_idx != nullptr ? a.rope_idx : a.row_idx};
 }
 
 }  // namespace oc

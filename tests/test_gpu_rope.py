@@ -7,7 +7,7 @@ import torch
 import paper_2607_23844_amd as oc
 from oc_synth import small_workload
 from ops_ref import check, d, grid_pos, rope
-from parity import check_output_bars, dev_tensor, rel_err, shapes, to_f64, weights_dev, weights_f64
+from parity import TOL, check_output_bars, dev_tensor, rel_err, shapes, to_f64, weights_dev, weights_f64
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -248,30 +248,64 @@ def test_layer(i):
         bars(yf[q], ref[:len(q)], dt, "uncached rows")
 
 
+def reduced(rp, L, n_seq, heads, dh, n_ctx=0, C=128):
+    """attn_reduced of random rows, some of them without a token (not turned), against 64 bits."""
+    sh = oc.Shape(**GRID, C=C, heads=heads, head_dim=dh, n_ctx=n_ctx)
+    n, hd = sh.F * sh.N, heads * dh
+    g = torch.Generator().manual_seed(L)
+    W64 = {k: torch.randn(hd, C, generator=g, dtype=torch.float64) / C ** 0.5 for k in ("wq", "wk", "wv")}
+    W64["wo"] = torch.randn(C, hd, generator=g, dtype=torch.float64) / hd ** 0.5
+    W = {k: v.bfloat16().to(DEV) for k, v in W64.items()}
+    W64 = {k: v.cpu().double().numpy() for k, v in W.items()}
+    x = torch.randn(n_seq * L, C, generator=g).bfloat16()
+    ctx = torch.randn(n_ctx, C, generator=g).bfloat16() if n_ctx else None
+    idx = torch.randint(0, n, (n_seq * L,), generator=g, dtype=torch.int32)
+    idx[::7] = n
+    idx[3::11] = -1
+    y, yc = oc.attn_reduced(x.to(DEV), n_seq, L, W, sh, ctx=None if ctx is None else ctx.to(DEV), rope=rp,
+                            kept_idx=idx.to(DEV))
+    there = (idx >= 0) & (idx < n)
+    pos = grid_pos(torch.where(there, idx, 0).long(), sh.H, sh.W)
+    pos[~there] = 0   # (the angle at the origin is nothing)
+    c64 = None if ctx is None else ctx.double().numpy()
+    ref = np.concatenate([attention(x[i:i + L].double().numpy(), c64, pos[i:i + L], W64, heads, dh, rp)
+                          for i in range(0, n_seq * L, L)])
+    y = to_f64(y if yc is None else torch.cat([y, yc])).reshape(ref.shape)
+    # The computation's error by the layer's bar.  Beside it the outputs' rounding, at most 2^-8 of a value, so 2^-8 of
+    # the largest one in the unadjusted error (among millions of outputs that is 6 times their RMS: 0.0235).
+    assert rel_err(y, ref, "bf16") <= TOL["bf16"]
+    assert rel_err(y, ref) <= TOL["bf16"] + 2.0 ** -8 * np.abs(ref).max() / np.sqrt(np.mean(ref * ref))
+
+
+@pytest.mark.parametrize("L,n_seq,n_ctx", [(300, 1, 21), (90, 3, 0), (40, 7, 0)])
+@pytest.mark.parametrize("heads,dh,rp", [
+    (5, 72, oc.Rope((24, 24, 24))), (5, 72, oc.Rope((24, 24, 24), layout="halves")),
+    (3, 128, oc.Rope((32, 48, 48), layout="halves")), (5, 64, oc.Rope((0, 32, 32), layout="split")),
+    (6, 48, oc.Rope((16, 8, 8))), (3, 96, oc.Rope((32, 32, 32), layout="halves")),
+    (7, 80, oc.Rope((14, 10, 22))), (9, 32, oc.Rope((8, 8, 16), layout="halves")), (17, 16, oc.Rope((0, 8, 8))),
+    (4, 128, oc.Rope((40, 40, 8), layout="split", shared=True)), (4, 64, oc.Rope((64, 0, 0))),
+])
+def test_reduced_sequences(L, n_seq, n_ctx, heads, dh, rp):
+    """Heads and halves inside and across the tiles of the projection."""
+    reduced(rp, L, n_seq, heads, dh, n_ctx)
+
+
+@pytest.mark.parametrize("C,L,n_seq,n_ctx,heads,dh", [(1536, 2048, 1, 333, 24, 64), (1152, 256, 12, 0, 16, 72),
+                                                      (320, 90, 222, 0, 5, 64), (640, 512, 16, 0, 10, 64),
+                                                      (1024, 128, 4, 0, 8, 128), (1152, 16, 150, 0, 16, 72)])
+@pytest.mark.parametrize("layout", ["pairs", "halves"])
+def test_large_projections(layout, C, L, n_seq, n_ctx, heads, dh):
+    """The large tiles' rotation."""
+    reduced(oc.Rope((16, 24, 24), layout=layout), L, n_seq, heads, dh, n_ctx, C)
+
+
 @pytest.mark.parametrize("L,n_seq", [(1, 130), (3, 43), (25, 11), (64, 3)])
 @pytest.mark.parametrize("rp", [oc.Rope((64, 0, 0)), oc.Rope((16, 24, 24), layout="halves", shared=True),
                                 oc.Rope((14, 10, 22)), oc.Rope((14, 10, 22), layout="halves"),
                                 oc.Rope((6, 0, 4), layout="split")])
 def test_short_sequences(rp, L, n_seq):
     """Heads of 64 and few tokens a sequence; rows without a token are not turned."""
-    sh = oc.Shape(**GRID, C=128, heads=3, head_dim=64)
-    n = sh.F * sh.N
-    g = torch.Generator().manual_seed(L)
-    W64 = {k: torch.randn(192, 128, generator=g, dtype=torch.float64) / 128 ** 0.5 for k in ("wq", "wk", "wv")}
-    W64["wo"] = torch.randn(128, 192, generator=g, dtype=torch.float64) / 192 ** 0.5
-    W = {k: v.bfloat16().to(DEV) for k, v in W64.items()}
-    W64 = {k: v.cpu().double().numpy() for k, v in W.items()}
-    x = torch.randn(n_seq * L, 128, generator=g).bfloat16()
-    idx = torch.randint(0, n, (n_seq * L,), generator=g, dtype=torch.int32)
-    idx[::7] = n
-    idx[3::11] = -1
-    y, _ = oc.attn_reduced(x.to(DEV), n_seq, L, W, sh, rope=rp, kept_idx=idx.to(DEV))
-    there = (idx >= 0) & (idx < n)
-    pos = grid_pos(torch.where(there, idx, 0).long(), sh.H, sh.W)
-    pos[~there] = 0   # (the angle at the origin is nothing)
-    ref = np.concatenate([attention(x[i:i + L].double().numpy(), None, pos[i:i + L], W64, 3, 64, rp)
-                          for i in range(0, n_seq * L, L)])
-    bars(to_f64(y).reshape(ref.shape), ref, "bf16", "rows")
+    reduced(rp, L, n_seq, 3, 64)
 
 
 def test_staged_calls_and_runner_match_the_layer_call():
