@@ -356,17 +356,18 @@ __global__ __launch_bounds__(RING_THREADS<ID>) void k_linear_i8(LinearI8Args a, 
 
 // ---------------------------------------------------------------------------
 // The product of few rows: bound by the weights' way from HBM, so a block takes
-// 16 weight rows and all its waves share out their K (the ring's tiles would be
-// N / 64 blocks of one after another 128 bytes).  v_mfma_i32_16x16x64_i8, a =
-// weights, b = up to 16 RT batch rows, four of them from one round of loads.
-// The waves' sums are added in LDS (integers: in any order).
+// 16 weight rows (or OUT = 8, half of an MFMA's) and all its waves share out
+// their K (the ring's tiles would be N / 64 blocks of one after another 128
+// bytes).  v_mfma_i32_16x16x64_i8, a = weights, b = up to 16 RT batch rows, four
+// of them from one round of loads.  The waves' sums are added in LDS (integers:
+// in any order).
 // ---------------------------------------------------------------------------
-template <typename T, int RT>
+template <typename T, int RT, int OUT>
 __global__ __launch_bounds__(1024) void k_linear_i8_thin(LinearI8Args a) {
     extern __shared__ __align__(16) int part[];   // [wave][RT][16 batch rows][16 + 4 outputs]
     constexpr int LD = 20;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
-    const int lr = lane & 15, lg = lane >> 4, n0 = blockIdx.x * 16;
+    const int lr = lane & 15, lg = lane >> 4, n0 = blockIdx.x * OUT;
     const int Kp = (a.K + 15) & ~15;
     const int8_t *w = a.w + (long)min(n0 + lr, a.N - 1) * Kp;
     const int8_t *q[RT];
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(1024) void k_linear_i8_thin(LinearI8Args a) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const int k = k0 + s * 64 + lg * 16;
-            fw[s] = k < Kp ? *reinterpret_cast<const i32x4 *>(w + k) : zero;
+            fw[s] = k < Kp && (OUT == 16 || lr < OUT) ? *reinterpret_cast<const i32x4 *>(w + k) : zero;
 #pragma unroll
             for (int t = 0; t < RT; ++t) fq[t][s] = k < Kp ? *reinterpret_cast<const i32x4 *>(q[t] + k) : zero;
         }
@@ -397,8 +398,8 @@ __global__ __launch_bounds__(1024) void k_linear_i8_thin(LinearI8Args a) {
     for (int t = 0; t < RT; ++t)
         *reinterpret_cast<i32x4 *>(part + ((wave * RT + t) * 16 + lr) * LD + lg * 4) = acc[t];
     __syncthreads();
-    for (int i = threadIdx.x; i < RT * 64; i += blockDim.x) {
-        const int r = i >> 2, n = (i & 3) * 4;
+    for (int i = threadIdx.x; i < RT * 4 * OUT; i += blockDim.x) {
+        const int r = i / (OUT / 4), n = i % (OUT / 4) * 4;
         const long o = out_row(a, r);
         if (o < 0 || n0 + n >= a.N) continue;
         i32x4 s = zero;
@@ -412,15 +413,24 @@ __global__ __launch_bounds__(1024) void k_linear_i8_thin(LinearI8Args a) {
     }
 }
 
+template <typename T, int RT, int OUT>
+hipError_t go_thin_out(const LinearI8Args &a, hipStream_t st) {
+    // waves: one pass of 256 bytes of k each, or as few as 16 waves need
+    const int blocks = cdiv(a.N, OUT), passes = cdiv(a.K, 256), nw = cdiv(passes, cdiv(passes, 16));
+    const size_t lds = (size_t)nw * RT * 16 * 20 * 4;
+    const hipError_t e = raise_lds_limit((const void *)k_linear_i8_thin<T, RT, OUT>, lds);
+    if (e != hipSuccess) return e;
+    launch_k(k_linear_i8_thin<T, RT, OUT>, (unsigned)blocks, nw * 64, lds, st, a);
+    return hipGetLastError();
+}
+
 template <typename T, int RT>
 hipError_t go_thin(const LinearI8Args &a, hipStream_t st) {
-    // waves: one pass of 256 bytes of k each, or as few as 16 waves need
-    const int blocks = cdiv(a.N, 16), passes = cdiv(a.K, 256), nw = cdiv(passes, cdiv(passes, 16));
-    const size_t lds = (size_t)nw * RT * 16 * 20 * 4;
-    const hipError_t e = raise_lds_limit((const void *)k_linear_i8_thin<T, RT>, lds);
-    if (e != hipSuccess) return e;
-    launch_k(k_linear_i8_thin<T, RT>, (unsigned)blocks, nw * 64, lds, st, a);
-    return hipGetLastError();
+    // Eight outputs a block where these are no more blocks than units and rows are long: what bounds a block
+    // is then its own weights' way (one row of K = 6144, N = 1536 5.6 us against 6.6, 32 rows 10.4 against
+    // 11.2, K = 1536 3.8 against 3.9; past that the rows' second reading costs more, N = 3200 4.5 against 4.1,
+    // and with K = 320 2.6 against 2.5).
+    return a.N <= 8 * N_CUS && a.K >= 1024 ? go_thin_out<T, RT, 8>(a, st) : go_thin_out<T, RT, 16>(a, st);
 }
 
 // The tile shapes' costs for this product (as RING_SHAPES; its epilogue is
@@ -454,9 +464,9 @@ hipError_t go_ring(const LinearI8Args &a, hipStream_t st) {
 
 template <typename T>
 hipError_t go_linear(const LinearI8Args &a, hipStream_t st) {
-    // Up to 16 rows: 3.9 us against the ring's 6.7 for one row of K = N = 1536, 6.3 against 8.5 at N =
-    // 9216.  Up to 32 while the ring's tiles of 64 outputs are few: 32 rows, K = 1536, N = 1536 5.2
-    // against 6.8, N = 4608 7.3 against 7.0 (every block reads all rows from L2).
+    // Up to 16 rows: 3.8 us against the ring's 6.3 for one row of K = N = 1536, 6.3 against 7.8 at N =
+    // 9216.  Up to 32 while the ring's tiles of 64 outputs are few: 32 rows, K = 1536, N = 1536 5.1
+    // against 6.4, N = 4608 7.3 against 6.5 (every block reads all rows from L2).
     if (a.rows <= 16) return go_thin<T, 1>(a, st);
     if (a.rows <= 32 && a.N <= 4096) return go_thin<T, 2>(a, st);
     return a.gelu ? go_ring<T, true>(a, st) : go_ring<T, false>(a, st);

@@ -123,6 +123,13 @@ def test_product(rows, K, N, dtype):
         check(y, *linear_i8(q, s, w, ws, b, act), N_ROUND, act)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,K,N", [(1, 1024, 8), (16, 1032, 2048), (5, 1016, 2048), (5, 2048, 2056), (20, 320, 1000),
+                                      (32, 1536, 2056), (32, 6144, 1544), (17, 1024, 24), (32, 72, 4096), (17, 200, 4104)])
+def test_product_of_few_rows(rows, K, N, dtype):
+    test_product(rows, K, N, dtype)
+
+
 @pytest.mark.parametrize("rows", [1, 16, 200])
 def test_sums_are_exact_integers(rows):
     """The largest sums that fit (-128 too), and sums that fp32 would not hold."""
