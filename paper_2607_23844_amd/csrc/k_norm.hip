@@ -961,8 +961,9 @@ hipError_t launch_norm_gate(const NormArgs &a, void *h, void *n, hipStream_t st)
 
 static_assert(sizeof(RowStats) == GRAD_ROW_STATS, "the plan's statistics");
 
-size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod) {
-    return rows > 0 ? grad_plan(rows, C, rows_per_mod > 0 ? rows_per_mod : rows, rows_per_mod > 0, true).bytes() : 0;
+size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod, bool bf16) {
+    if (rows <= 0) return 0;
+    return grad_plan(rows, C, rows_per_mod > 0 ? rows_per_mod : rows, rows_per_mod > 0, true, bf16).bytes();
 }
 
 template <typename T, int TPR, int CH, bool SUMS, bool ALONE>
@@ -1000,7 +1001,7 @@ template <typename T>
 static hipError_t type_norm_grad(const NormArgs &a, const T *dh, const T *dn, T *dx, T *dy, const NormGrads &q,
                                  void *ws, hipStream_t st) {
     const bool mods = q.gate || q.scale || q.shift, vecs = q.post_w || q.post_b || q.pre_w || q.pre_b;
-    const GradPlan p = grad_plan(a.rows, a.C, a.rows_per_mod, mods, vecs);
+    const GradPlan p = grad_plan(a.rows, a.C, a.rows_per_mod, mods, vecs, a.bf16);
     return with_team(p.team, [&](auto tpr, auto ch) -> hipError_t {
         constexpr int TPR = decltype(tpr)::value, CH = decltype(ch)::value;
         if constexpr (CH == 0) {

@@ -41,11 +41,19 @@ inline NormTeam grad_team(int rows, int C) {
     return {256, c <= 512 ? 2 : c <= 1024 ? 4 : 0};
 }
 
-// Most blocks of a gradient call: those that run at once, two on a unit, or one
-// where three or four chunks take its registers (another round would pay again
-// for a block's products and sums: 8192 x 1152 45 us by 512 blocks, 41 by 256).
-constexpr int GRAD_BLOCKS = 2 * NORM_CUS;
-inline int grad_most_blocks(NormTeam t) { return t.chunks > 2 ? NORM_CUS : GRAD_BLOCKS; }
+// Most blocks of a gradient call: those that run at once (another round would
+// pay again for a block's products and sums: 8192 x 1152 45 us by 512 blocks, 41
+// by 256).  One on a unit where a thread's chunks take its registers (from three,
+// from two of fp32 of the block: 4000 x 2496 in fp32 50 us by 256, 55 by 512) and
+// where the block has few rows (300 x 1704 with all vectors 17 us by 150 blocks
+// of two rows, 22 by 300), three where it has many of one bf16 chunk (16000 x
+// 1704 62 us by 768, 74 by 512; in fp32 98 and 97), else two.
+constexpr int GRAD_BLOCKS = 3 * NORM_CUS;
+inline int grad_most_blocks(NormTeam t, int rows, bool bf16) {
+    const bool block = t.threads == 256;
+    if (t.chunks > 2 || (block && (rows <= 4 * NORM_CUS || (t.chunks == 2 && !bf16)))) return NORM_CUS;
+    return block && t.chunks == 1 && bf16 && rows >= 32 * NORM_CUS ? 3 * NORM_CUS : 2 * NORM_CUS;
+}
 
 // Item i of n_items: rows [start, start + part) of modulation row i / per_group,
 // part i % per_group of it.  alone: a team takes an item by itself, else the
@@ -62,27 +70,28 @@ struct GradPlan {
 };
 constexpr size_t GRAD_ROW_STATS = 24;   // bytes of a long row's statistics
 
-inline GradPlan grad_plan(int rows, int C, int rows_per_mod, bool mods, bool vecs) {
+inline GradPlan grad_plan(int rows, int C, int rows_per_mod, bool mods, bool vecs, bool bf16 = true) {
     auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
     auto div = [](int a, int b) { return (a + b - 1) / b; };
     GradPlan g{};
     g.team = grad_team(rows, C);
     if (g.team.chunks == 0) {
-        g.part = div(rows, GRAD_BLOCKS);
+        g.part = div(rows, 2 * NORM_CUS);
         g.per_group = 1;
         g.n_items = g.blocks = div(rows, g.part);
         g.stats = up((size_t)rows * GRAD_ROW_STATS);
         g.slots = mods ? up(6 * (size_t)g.n_items * C * 4) : 0;
     } else {
+        const int most = grad_most_blocks(g.team, rows, bf16);
         const int teams = 256 / g.team.threads, per = std::min(rows_per_mod, rows), n_mod = div(rows, per);
         g.alone = teams > 1 && per < std::max(2 * teams, 16);
         // (an item's sums cost its share of LDS and of the join: four rows a team where that leaves no unit idle)
         const int least = std::min(std::max(rows / (NORM_CUS * teams), 1), 4) * teams;
-        g.per_group = g.alone ? 1 : std::min(std::max(1, grad_most_blocks(g.team) / n_mod), div(per, least));
+        g.per_group = g.alone ? 1 : std::min(std::max(1, most / n_mod), div(per, least));
         g.part = div(per, g.per_group);
         g.per_group = div(per, g.part);
         g.n_items = n_mod * g.per_group;
-        g.blocks = std::min(g.alone ? div(g.n_items, teams) : g.n_items, grad_most_blocks(g.team));
+        g.blocks = std::min(g.alone ? div(g.n_items, teams) : g.n_items, most);
         g.slots = mods && g.per_group > 1 ? up(3 * (size_t)g.n_items * C * 4) : 0;
     }
     g.sums = vecs ? up(4 * (size_t)g.blocks * C * 4) : 0;

@@ -207,7 +207,7 @@ oc_status oc_norm_gate(const oc_shape *shape, int32_t n_rows, const void *x, con
 
 size_t oc_norm_gate_grad_workspace_bytes(const oc_shape *shape, int32_t n_rows, int32_t rows_per_mod) {
     if (valid_shape(shape) != OC_OK || n_rows < 0 || n_rows >= (1 << 30) || rows_per_mod < 0) return 0;
-    return norm_grad_workspace_bytes(n_rows, shape->C, rows_per_mod);
+    return norm_grad_workspace_bytes(n_rows, shape->C, rows_per_mod, shape->dtype == OC_BF16);
 }
 
 oc_status oc_norm_gate_grad(const oc_shape *shape, int32_t n_rows, const void *x, const void *y, const oc_norm *post,
@@ -232,7 +232,7 @@ oc_status oc_norm_gate_grad(const oc_shape *shape, int32_t n_rows, const void *x
     if (!is_aligned(dh, 16) || !is_aligned(dn, 16) || !is_aligned(dx, 16) || !is_aligned(dy, 16))
         return failf(OC_ERR_INVALID_ARG, "dh, dn, dx and dy must be 16-byte aligned");
     const size_t esz = a.bf16 ? 2 : 4, bytes = (size_t)n_rows * a.C * esz;
-    const size_t need = norm_grad_workspace_bytes(n_rows, a.C, mod ? mod->rows_per_mod : 0);
+    const size_t need = norm_grad_workspace_bytes(n_rows, a.C, mod ? mod->rows_per_mod : 0, a.bf16);
     if ((s = valid_ws(ws, ws_bytes, need)) != OC_OK) return s;
     // outputs against inputs, the vectors, the workspace and each other
     Range v[7];

@@ -24,7 +24,7 @@ hipError_t launch_norm_gate(const NormArgs &a, void *h, void *n, hipStream_t st)
 hipError_t launch_norm_gate_grad(const NormArgs &a, const void *dh, const void *dn, void *dx, void *dy,
                                  const NormGrads &g, void *ws, hipStream_t st);
 hipError_t launch_zero(float *p, int n, hipStream_t st);   // gradients summed over no rows
-size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod);
+size_t norm_grad_workspace_bytes(int rows, int C, int rows_per_mod, bool bf16);
 
 
 // Rotary positions, the geometry of one head as a kernel takes it: pairs 0..P

@@ -9,8 +9,8 @@
 
 using namespace oc;
 
-static int check(int rows, int C, int per, bool mods, bool vecs) {
-    const GradPlan g = grad_plan(rows, C, per, mods, vecs);
+static int check(int rows, int C, int per, bool mods, bool vecs, bool bf16) {
+    const GradPlan g = grad_plan(rows, C, per, mods, vecs, bf16);
     const int T = 256 / g.team.threads;
     auto bad = [&](const char *what) {
         std::printf("%s: rows %d C %d per %d mods %d vecs %d: part %d per_group %d items %d blocks %d\n", what, rows, C,
@@ -47,14 +47,14 @@ static int check(int rows, int C, int per, bool mods, bool vecs) {
     if (mods && (g.team.chunks == 0 || g.per_group > 1) && g.slots < slot) return bad("slots");
     if (vecs && g.sums < 4 * (size_t)g.blocks * C * 4) return bad("sums");
     if (g.team.chunks == 0 && (g.stats < (size_t)rows * GRAD_ROW_STATS || g.blocks != g.n_items)) return bad("stats");
-    if (T > 1 && g.alone && (long)g.blocks * T < std::min<long>(g.n_items, (long)grad_most_blocks(g.team) * T)) return bad("teams");
+    if (T > 1 && g.alone && (long)g.blocks * T < std::min<long>(g.n_items, (long)grad_most_blocks(g.team, rows, bf16) * T)) return bad("teams");
     // the size that callers are told covers every choice of gradients
     oc_shape sh;
     std::memset(&sh, 0, sizeof(sh));
     sh.F = sh.H = sh.W = sh.heads = 1;
     sh.head_dim = 16;
     sh.C = C;
-    sh.dtype = OC_BF16;
+    sh.dtype = bf16 ? OC_BF16 : OC_F32;
     if (mods && oc_norm_gate_grad_workspace_bytes(&sh, rows, per) < g.bytes()) return bad("workspace");
     if (!mods && per >= rows && oc_norm_gate_grad_workspace_bytes(&sh, rows, 0) < g.bytes()) return bad("workspace (no modulation)");
     return 0;
@@ -66,6 +66,6 @@ int main() {
         for (int rows : {1, 2, 3, 4, 5, 7, 15, 16, 17, 31, 100, 255, 256, 511, 512, 513, 1023, 1024, 1025, 1500, 2047, 4096,
                          4429, 20000})
             for (int per : {1, 2, 3, 4, 5, 7, 8, 15, 16, 17, 31, 32, 33, 40, 100, 256, 511, 513, 1024, 4096, 9216, 1 << 30})
-                for (int w = 0; w < 4; ++w) rc |= check(rows, C, per, w & 1, w & 2);
+                for (int w = 0; w < 8; ++w) rc |= check(rows, C, per, w & 1, w & 2, w & 4);
     return rc;
 }
