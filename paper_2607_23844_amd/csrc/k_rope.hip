@@ -1,10 +1,10 @@
 // Rotary positions of q and k rows with up to three axes.
 //
 // A block turns `rows` rows.  First the cosines and sines of its rows' pairs, one
-// per thread, into LDS (oc_rope.h).  Then all heads of q and k of those rows, in units of 8 neighbouring channels (pairs side by
-// side) or of V channels and their V partners half a section further;
-// consecutive threads take consecutive units, four of them loaded at a time.
-// Bound by q's and k's way through HBM.
+// per thread, into LDS (oc_rope.h).  Then all heads of q and k of those rows, in
+// units of 8 neighbouring channels (pairs side by side) or of V channels and
+// their V partners half a section further; consecutive threads take consecutive
+// units, four of them loaded at a time.  Bound by q's and k's way through HBM.
 #include "oc_attn_common.h"
 #include "oc_device.h"
 #include "oc_launch.h"
