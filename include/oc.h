@@ -514,7 +514,8 @@ oc_status oc_rope_qk(const oc_shape *shape, const oc_rope *rope, int32_t n_rows,
  * exactly the call without it.  oc_attn_reduced_rope takes the tokens of its
  * rows: kept_idx [n_seq * seq_len], as oc_gather got it (rows outside [0, F*N)
  * are not turned).  bf16 layers hold q and k in fp16 before and after the
- * rotation (a second rounding of 2^-11).  Workspaces as without _rope.
+ * rotation (a second rounding of 2^-11; saturated at +-65504 both times).
+ * Workspaces as without _rope.
  * (oc_layer_cached_static and oc_block_cached have no such form: a block with
  * positions is two oc_layer_cached_rope calls and
  * oc_residual_add or oc_norm_gate between them.)

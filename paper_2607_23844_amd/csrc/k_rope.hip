@@ -30,7 +30,7 @@ __device__ __forceinline__ void put(T *p, const float (&v)[V]) {
     typedef typename Chunk<T, V>::type C;
     C c;
 #pragma unroll
-    for (int i = 0; i < V; ++i) c[i] = (T)v[i];
+    for (int i = 0; i < V; ++i) c[i] = turned<T>(v[i]);
     *reinterpret_cast<C *>(p) = c;
 }
 
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(256) void k_rope_lds(RopeGeom g, RopeArgs a, int bl
                 T &x = data[s * g.dh + lo], &y = data[s * g.dh + hi];
                 float u = (float)x, v = (float)y;
                 turn_pair(u, v, t);
-                x = (T)u;
-                y = (T)v;
+                x = turned<T>(u);
+                y = turned<T>(v);
             }
         }
         __syncthreads();

@@ -3,6 +3,7 @@
 #pragma once
 #include "oc_device.h"
 #include "oc_internal.h"
+#include "oc_mfma_tile.h"
 #include "oc_ops.h"
 #include <type_traits>
 
@@ -46,6 +47,14 @@ __device__ __forceinline__ void turn_pair(float &x, float &y, const Turn &t) {
     y = fmaf(x0, t.s, y0 * t.c);
 }
 
+// A turned value in its tensor's type; fp16 saturates as the projections do: a pair
+// inside its range can be turned out of it, up to sqrt(2) 65504.
+template <typename T>
+__device__ __forceinline__ T turned(float v) {
+    if constexpr (std::is_same<T, _Float16>::value) return __builtin_bit_cast(_Float16, f2h_bits(v));
+    else return (T)v;
+}
+
 // V pairs of a head, from pair p0 on (all of them turned), staged in LDS in fp16:
 // a run of 2 V channels, or two of V.  V = 1, or 4 where it divides the sections
 // (vec).
@@ -86,8 +95,8 @@ struct RopeUnit {
     __device__ __forceinline__ static void apply(Vals &v, int j, const Turn &t) {
         float x = (float)v.a[PAIRS ? 2 * j : j], y = PAIRS ? (float)v.a[PAIRS ? 2 * j + 1 : 0] : (float)v.b[j];
         turn_pair(x, y, t);
-        v.a[PAIRS ? 2 * j : j] = (_Float16)x;
-        (PAIRS ? v.a : v.b)[PAIRS ? 2 * j + 1 : j] = (_Float16)y;
+        v.a[PAIRS ? 2 * j : j] = turned<_Float16>(x);
+        (PAIRS ? v.a : v.b)[PAIRS ? 2 * j + 1 : j] = turned<_Float16>(y);
     }
 };
 
