@@ -441,12 +441,15 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
                     s2 = fmaf(t[i][e], u[i][e], s2);
                 }
             }
-            if (row < stop) fetch(dn, next, rn);
-            float m1 = 0.f, m2 = 0.f;
+            if (!ALONE && row < stop) fetch(dn, next, rn);
+            // (without a norm H does not hold u, which may be infinite)
             if (a.pre != 0) {
                 Team<TPR>::sum2(s1, s2, red);
-                m1 = a.pre == NORM_LAYER ? s1 * per_c : 0.f;
-                m2 = s2 * per_c;
+                const float m1 = a.pre == NORM_LAYER ? s1 * per_c : 0.f, m2 = s2 * per_c;
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) t[i][e] = fmaf(-u[i][e], m2, t[i][e] - m1);
             }
             // t becomes H
 #pragma unroll
@@ -455,12 +458,15 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
                 widen(rh[i], o);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    t[i][e] = fmaf(r_h, fmaf(-u[i][e], m2, t[i][e] - m1), o[e]);
+                    t[i][e] = fmaf(r_h, t[i][e], o[e]);
                     o[e] = rs * t[i][e];
                 }
                 if (dx != nullptr && r.in(i)) store8(dx + at + r.at(i), o);
             }
-            if (row < stop) fetch(dh, next, rh);
+            if (row < stop) {
+                if (ALONE) fetch(dn, next, rn);   // (few next rows, many registers)
+                fetch(dh, next, rh);
+            }
             if (a.y == nullptr) continue;
             s1 = s2 = 0.f;
 #pragma unroll
@@ -744,8 +750,13 @@ struct GradRow : NormRow<T> {
         inner(c, u, av, da);
         load8_or((const T *)a.pre_w, c, 1.f, w);
         load8_or(dh, at + c, 0.f, H);
+        if (a.pre != 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) H[i] = fmaf(sh.rstd, fmaf(da[i], w[i], -m1) - u[i] * m2, H[i]);
+            for (int i = 0; i < 8; ++i) H[i] = fmaf(sh.rstd, fmaf(da[i], w[i], -m1) - u[i] * m2, H[i]);
+        } else {   // (H does not hold u, which may be infinite)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) H[i] = fmaf(sh.rstd, fmaf(da[i], w[i], -m1), H[i]);
+        }
     }
 };
 
@@ -800,8 +811,10 @@ __global__ __launch_bounds__(256) void k_norm_grad_rows_wide(NormArgs a, const T
     for (int c = threadIdx.x * 8; c < a.C; c += 2048) {
         if (dy != nullptr) {
             inner_y(c, H, v, d);
+            if (a.post != 0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) d[i] = r.sy.rstd * (d[i] - k1 - v[i] * k2);
+                for (int i = 0; i < 8; ++i) d[i] = r.sy.rstd * (d[i] - k1 - v[i] * k2);
+            }
             store8(dy + r.at + c, d);
         } else {
             r.stream_grad(c, H);
