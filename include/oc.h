@@ -336,7 +336,8 @@ oc_status oc_norm_gate(const oc_shape *shape, int32_t n_rows, const void *x, con
 
 /*
  * oc_norm_gate_grad — the gradient of oc_norm_gate: from dh and dn, the
- * gradients of h and n (either may be NULL: zero; not both), those of x (dx)
+ * gradients of h and n (either may be NULL: zero; not both; without dn nothing
+ * of n takes part, whatever the rows hold), those of x (dx)
  * and y (dy), [n_rows, C] each, in the tensors' type; and in fp32 those of the
  * vectors: gate, scale, shift [n_mod, C] (contiguous) and the norms' w and b
  * [C].  Each output may be NULL (not wanted), and must be where what it

@@ -496,6 +496,7 @@ __global__ __launch_bounds__(256) void k_norm_grad(NormArgs a, const T *dh, cons
             r.store(dy + at, t);
         }
         if constexpr (SUMS) {
+            if (dn == nullptr) clear(sum[0]);   // (no gradient times a u that may not be finite)
             // the sums of N channels from c on, to the gradients that they make
             auto emit = [&](int c, auto width, const float *sa, const float *sb, const float *sc, const float *sd) {
                 constexpr int N = decltype(width)::value;
@@ -853,15 +854,17 @@ __global__ __launch_bounds__(64) void k_norm_grad_cols_wide(NormArgs a, const T 
         r.sh = st.sh;
         r.m1 = st.m1;
         r.m2 = st.m2;
-        float u[8], av[8], da[8], d[8];
-        r.inner(c, u, av, da);
-        load8_or(dn, r.at + c, 0.f, d);
+        if (dn != nullptr) {
+            float u[8], av[8], da[8], d[8];
+            r.inner(c, u, av, da);
+            load8(dn + r.at + c, d);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            q[Q_SCALE][i] = fmaf(d[i], av[i], q[Q_SCALE][i]);
-            q[Q_SHIFT][i] += d[i];
-            q[Q_PREW][i] = fmaf(da[i], u[i], q[Q_PREW][i]);
-            q[Q_PREB][i] += da[i];
+            for (int i = 0; i < 8; ++i) {
+                q[Q_SCALE][i] = fmaf(d[i], av[i], q[Q_SCALE][i]);
+                q[Q_SHIFT][i] += d[i];
+                q[Q_PREW][i] = fmaf(da[i], u[i], q[Q_PREW][i]);
+                q[Q_PREB][i] += da[i];
+            }
         }
         if (a.y != nullptr) {
             float H[8], v[8], z[8], g[8];
@@ -1036,9 +1039,14 @@ static hipError_t type_norm_grad(const NormArgs &a, const T *dh, const T *dn, T 
     });
 }
 
-hipError_t launch_norm_gate_grad(const NormArgs &a, const void *dh, const void *dn, void *dx, void *dy,
+hipError_t launch_norm_gate_grad(const NormArgs &args, const void *dh, const void *dn, void *dx, void *dy,
                                  const NormGrads &q, void *ws, hipStream_t st) {
     StageScope _stage(st, "norm_gate_grad");
+    NormArgs a = args;
+    if (dn == nullptr) {   // n takes no part: its norm is not made, whatever the rows hold
+        a.pre = 0;
+        a.pre_w = a.pre_b = a.scale = nullptr;
+    }
     if (a.bf16)
         return type_norm_grad(a, (const uint16_t *)dh, (const uint16_t *)dn, (uint16_t *)dx, (uint16_t *)dy, q, ws, st);
     return type_norm_grad(a, (const float *)dh, (const float *)dn, (float *)dx, (float *)dy, q, ws, st);

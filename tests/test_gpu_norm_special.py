@@ -44,3 +44,20 @@ def test_no_norm_after_and_infinite_sublayer_output(rows, C, dtype):
     out = oc.norm_gate_grad(x, shape(C, dtype), dh=dh, want=("dx", "dy"), **kw)
     for k in ("dx", "dy"):
         check(out[k], *want[k], BWD, k)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("per", [1, 5, 600])
+@pytest.mark.parametrize("rows,C", SIZES)
+def test_rows_that_are_not_finite_where_n_has_no_gradient(rows, C, per, dtype):
+    """dn NULL: n takes no part, whatever the rows hold.  dx = rs dh, dy and the
+    vectors of the norm after follow from H = dh, those of n are zero."""
+    x, kw, ref = setup(rows, C, dtype, pre="layer", post="rms", affine=True, per=per, rs=0.5)
+    dh = make(rows, C, dtype, 7)
+    want = ref.grads(dh)
+    x[3, 5], x[rows - 1, C - 1], x[rows // 2] = float("inf"), float("nan"), float("nan")
+    out = oc.norm_gate_grad(x, shape(C, dtype), dh=dh, **kw)
+    for k in ("scale", "shift", "pre_w", "pre_b"):
+        assert (out[k] == 0).all(), k
+    for k in ("dx", "dy", "gate", "post_w", "post_b"):
+        check(out[k], *(t.reshape(out[k].shape) for t in want[k]), BWD + (0 if k in ("dx", "dy") else rows), k)
