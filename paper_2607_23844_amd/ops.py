@@ -117,7 +117,9 @@ def _mod(m: Optional[Mod], rows: int, shape: Shape, dev) -> Optional[L.oc_mod]:
         if t.device != dev:
             raise _bad(L.OC_ERR_INVALID_ARG, f"{name} is on {t.device}, expected {dev}")
         size, step = t.shape, t.stride()
-        if size != (n_mod, Ch) and not (n_mod == 1 and size == (Ch,)):
+        # (no rows: the vector of all of them is one all the same)
+        if size != (n_mod, Ch) and not ((n_mod == 1 and size == (Ch,)) or (
+                rows == 0 and m.rows_per_mod is None and size in ((1, Ch), (Ch,)))):
             raise _bad(L.OC_ERR_SHAPE, f"{name} has shape {tuple(size)}, expected {(n_mod, Ch)}")
         if step[-1] != 1:
             raise _bad(L.OC_ERR_INVALID_ARG, f"the channels of {name} must be contiguous")
@@ -211,6 +213,10 @@ def norm_gate_grad(x: torch.Tensor, shape: Shape, dn: Optional[torch.Tensor] = N
             base, step = block.data_ptr(), block.stride(0) * 4
             for i, (k, t) in enumerate(zip(names, block.unbind(0))):
                 out[k], at[k] = t, base + i * step
+    if rows == 0:      # (nothing is written where there are no modulation rows)
+        for k in has:
+            if k in GRADS[2:5]:
+                out[k], at[k] = x.new_zeros((getattr(mod, k).numel() // shape.C, shape.C), dtype=torch.float32), None
     for k, there in (("dx", True), ("dy", y is not None)):
         if there and (want is None or k in want):
             out[k] = torch.empty_like(x)
