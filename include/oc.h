@@ -345,7 +345,7 @@ oc_status oc_norm_gate(const oc_shape *shape, int32_t n_rows, const void *x, con
  * forward call; statistics, h and z are computed again from x and y, nothing
  * has to be kept.  Where y is NULL, dh is added to dx.  Sums over rows are
  * fp32 and taken in an order that depends on the sizes only.  No output may
- * overlap an input or another output.
+ * overlap an input or another output, and the workspace overlaps nothing.
  * ws_bytes >= oc_norm_gate_grad_workspace_bytes(shape, n_rows, rows_per_mod)
  * (rows_per_mod of mod, or 0 without one).
  */

@@ -252,6 +252,12 @@ oc_status oc_norm_gate_grad(const oc_shape *shape, int32_t n_rows, const void *x
             if (overlaps(outs[i].p, outs[i].bytes, v[j].p, v[j].bytes))
                 return failf(OC_ERR_INVALID_ARG, "the gradients must not overlap the vectors");
     }
+    for (int i = 0; i < 4; ++i)
+        if (overlaps(ws, need, ins[i].p, ins[i].bytes))
+            return failf(OC_ERR_INVALID_ARG, "the workspace must not overlap an input");
+    for (int i = 0; i < nv; ++i)
+        if (overlaps(ws, need, v[i].p, v[i].bytes))
+            return failf(OC_ERR_INVALID_ARG, "the workspace must not overlap the vectors");
     if (n_rows == 0) {
         // sums over no rows: the vectors of all rows are zero, there are no modulation rows
         for (float *p : {g.post_w, g.post_b, g.pre_w, g.pre_b})
