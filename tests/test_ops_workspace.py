@@ -10,7 +10,7 @@ WS = at(9)
 
 @pytest.mark.parametrize("kw", [
     dict(x=WS), dict(y=WS + 256), dict(dh=WS), dict(dn=WS + 256),
-    dict(m=mod(gate=WS)), dict(m=mod(scale=WS + 256)), dict(m=mod(shift=WS)),
+    dict(m=mod(WS, None, None)), dict(m=mod(None, WS + 256, None)), dict(m=mod(None, None, WS)),
     dict(post=L.oc_norm(1, 1e-6, WS, None)), dict(pre=L.oc_norm(1, 1e-6, None, WS + 256)),
 ])
 def test_norm_gate_grad_refuses(kw):
