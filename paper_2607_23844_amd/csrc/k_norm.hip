@@ -208,8 +208,9 @@ __global__ __launch_bounds__(256) void k_norm_gate(NormArgs a, T *h, T *n) {
     if (row >= a.rows) return;
     const Row r(a.C);
     const long at = row * a.C, mod = row / a.rows_per_mod * a.ld;
-    // All on their way before the first sum (30000 x 1536: 69 us, 95 with each vector read where it is
-    // used); but three chunks of fp32 would leave two waves to a SIMD (230400 x 320: 227 against 217).
+    // Rows and modulation on their way before the first sum (30000 x 1536: 69 us, 95 with each vector read where
+    // it is used), the norms' weights and biases after it; but three chunks of fp32 would leave two waves to a
+    // SIMD (230400 x 320: 227 against 217), there the modulation comes after it too.
     constexpr bool EARLY = sizeof(T) == 2 || CH <= 2;
     typename Row::Raws rx, ry, rg, rs, rt;
     r.fetch((const T *)a.x + at, rx);

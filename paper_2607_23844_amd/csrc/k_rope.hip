@@ -182,7 +182,10 @@ __global__ __launch_bounds__(256) void k_rope_lds(RopeGeom g, RopeArgs a, int bl
 
 template <typename T>
 hipError_t type_rope(const RopeGeom &g, const RopeArgs &a, hipStream_t st) {
-    // rows of a block: all that leave two blocks for every unit
+    // rows of a block: all that leave two blocks for every unit, since few units of a row leave threads idle (bf16,
+    // 230400 rows of 2 x 5 heads of 64 111 us by 16 rows, 136 by four, 274 by one; 57600 rows 30, 35 and 68).  Rows of
+    // many heads fill a block by themselves and would do with fewer (2 x 24 heads, 2048 rows 9.9 us by four, 8.5 by
+    // one; 4096 rows 15.2 by eight, 11.9 by two).
     int rows = 1;
     while (rows < ROPE_ROWS && a.rows / (2 * rows) >= 2 * N_CUS) rows *= 2;
     auto go = [&](auto kern) {

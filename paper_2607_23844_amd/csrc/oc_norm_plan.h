@@ -27,9 +27,10 @@ inline NormTeam norm_team(int rows, int C) {
     return {256, c <= 512 ? 2 : c <= 1024 ? 4 : 0};
 }
 
-// Gradients: in two chunks where 16, 32 or 64 lanes can hold that (a row's
-// values, gradients and sums take over 12 registers a channel; 230400 x 320:
-// 239 us by 16 lanes of three chunks, 282 by 32 of two), the block from 1537.
+// Gradients: 16 lanes up to 384 channels (in up to three chunks), 32 in two up to
+// 512, 64 in two up to 1024 and in three up to 1536, then the block (a row's
+// values, gradients and sums take over 12 registers a channel; 230400 x 320 with
+// both norms' weights: 198 us by 16 lanes of three chunks, 200 by 32 of two).
 inline NormTeam grad_team(int rows, int C) {
     const int c = (C + 7) / 8;
     if (c <= 192 && rows >= 4 * NORM_CUS) {
@@ -41,18 +42,25 @@ inline NormTeam grad_team(int rows, int C) {
     return {256, c <= 512 ? 2 : c <= 1024 ? 4 : 0};
 }
 
-// Most blocks of a gradient call: those that run at once (another round would
-// pay again for a block's products and sums: 8192 x 1152 45 us by 512 blocks, 41
-// by 256).  One on a unit where a thread's chunks take its registers (from three,
-// from two of fp32 of the block: 4000 x 2496 in fp32 50 us by 256, 55 by 512) and
-// where the block has few rows (300 x 1704 with all vectors 17 us by 150 blocks
-// of two rows, 22 by 300), three where it has many of one bf16 chunk (16000 x
-// 1704 62 us by 768, 74 by 512; in fp32 98 and 97), else two.
+// Most blocks of a gradient call: about those that run at once (another round
+// would pay again for a block's products and sums: 8192 x 1152 with both norms'
+// weights 42 us by 256 blocks, 52 by 512).  One on a unit where a thread's chunks
+// take its registers (from three, from two of fp32 of the block: 4000 x 2496 in
+// fp32, likewise, 67 us by 256, 78 by 512) and where the block has few rows (300 x
+// 1704 with all vectors 17 us by 150 blocks of two rows, 22 by 300), three where
+// it has many of one bf16 chunk (16000 x 1704 without y 64 us by 768, 74 by 512,
+// with y 80 and 86, with both norms' weights 94 and 102; 8192 rows with y 46 and
+// 49, 4000 with both norms' weights 40 and 37; in fp32 16000 rows 154 and 148),
+// else two.  (Teams that take a modulation row alone in two chunks hold one
+// block's registers a unit where vectors' sums are wanted, so that their 512
+// blocks take two rounds: a modulation row a token, both norms' weights, 20000 x
+// 200 55 us and 51 by 256, x 512 125 and 124, x 704 222 and 221.  In fp32 with
+// three chunks they spill 11 to 21 registers, the block with four 10.)
 constexpr int GRAD_BLOCKS = 3 * NORM_CUS;
 inline int grad_most_blocks(NormTeam t, int rows, bool bf16) {
     const bool block = t.threads == 256;
     if (t.chunks > 2 || (block && (rows <= 4 * NORM_CUS || (t.chunks == 2 && !bf16)))) return NORM_CUS;
-    return block && t.chunks == 1 && bf16 && rows >= 32 * NORM_CUS ? 3 * NORM_CUS : 2 * NORM_CUS;
+    return block && t.chunks == 1 && bf16 && rows >= 32 * NORM_CUS ? GRAD_BLOCKS : 2 * NORM_CUS;
 }
 
 // Item i of n_items: rows [start, start + part) of modulation row i / per_group,
